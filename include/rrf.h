@@ -351,9 +351,8 @@ rrf_status rrf_copy_matrix(rrf_dtype dtype, const void* src, int64_t lds,
  *                call's work on the stream is done.
  * Asynchronous on hip_stream; no allocation, so it can be captured into a
  * graph.  A matrix whose norm is not finite gives NaN throughout.
- * The iterates carry 22 bits for f32 and f16 matrices and for bf16 ones with a
- * short side up to 192, else 11 (and the mean effect of the other 11 where the
- * following steps amplify the rounding); sums are binary32, the norm binary64.
+ * The iterates carry 22 bits whatever the type, sums are binary32, the norm
+ * binary64.
  * ------------------------------------------------------------------------- */
 rrf_status rrf_orthogonalize_workspace(rrf_dtype dtype, int64_t m, int64_t n,
                                        int64_t batch, int momentum,

@@ -5,7 +5,7 @@
 // with coefficients (a, b, c) is
 //   A = X X^T,   P = a I + b A + c A^2,   X <- P X,
 // which maps every singular value x to a x + b x^3 + c x^5 and leaves the
-// singular vectors.  Every product is one launch of a tile product (ring.h,
+// singular vectors.  Every product is one launch of a tile product (wide.h,
 // split.h).  A and P are symmetric, so only the tiles on and below the
 // diagonal are formed and each is stored twice; A^2 turns into P in the
 // epilogue; a product with X stores X in both orders ([l][s] is the next
@@ -20,31 +20,20 @@
 // half, P X 2 r); a group of g steps 3 r + 4 g - 3.  Rounding A_k costs more
 // then: an error in it grows by at most (max |a + b x^2 + c x^4|)^2 a step up
 // to the next Gram product, so that growth is held to a limit (kGroupGain):
-// with the quintic up to three steps on 22 bits (s > 500; two below) and two on
-// 11 (s > 500).
+// with the quintic up to three steps (s > 500; two below).
 //
 // Representation of the iterates.  Singular values stay below a bound that
 // the host takes from the coefficients, so X, A and P are held in binary16
 // times a power of two that puts the bound just below 2^15: 11 bits on the
-// binary16 matrix rate, with no range to lose.  A value that needs more is
-// the sum of two such numbers (hi + lo, 22 bits) and a product of two of them
-// is three (hi hi + hi lo + lo hi), accumulated in binary32.
-//   f32 and f16 matrices: all of X, A, P as hi + lo.
-//   bf16 matrices: hi only, except where it would show in the result's 8
-//     bits: rounding X adds a small full-rank matrix, and the steps that
-//     follow multiply its (small) singular values by their a's, so X_k keeps
-//     its low part while the product of the remaining a's exceeds 16 (with the
-//     quintic of five equal steps: k = 1, 2).  That part is a random matrix,
-//     spread over all singular directions, and what the next product makes of
-//     it is close to what the mean of the product's eigenvalues would: instead
-//     of Q lo, the epilogue adds (trace Q / s) lo.  (Against 64 bits the two
-//     differ by less than 1 % of the error; without lo it is 2 to 8 times as
-//     large; the second product cost 190 us at 4096 x 11008.)  X_0 of a
-//     bf16 matrix is exact.  Rounding A or P only perturbs the left factor,
-//     which is not amplified; but it is a random matrix whose norm counts for
-//     more the smaller it is, and short sides up to 192 (bound by latency in
-//     any case: 17 us a step of 300 x 500 against 13) take two planes as f32
-//     does.
+// binary16 matrix rate, with no range to lose.  Every value is the sum of two
+// such numbers (hi + lo, 22 bits, two planes) and a product of two of them is
+// three (hi hi + hi lo + lo hi), accumulated in binary32.  That holds for bf16
+// matrices too, though the result keeps 8 bits: the steps multiply small
+// singular values, and with them what rounding adds there, by up to 3.4^5.  One
+// plane of 11 bits was 1.8 times as fast (4096 x 11008) and as exact on low
+// rank with noise, but had two to three times the error of binary32 steps where
+// a twentieth of the rows or columns, or of the singular values, carries the
+// matrix.
 
 #include "cost.h"
 #include "split.h"
@@ -62,25 +51,18 @@ namespace {
 constexpr int kMaxSteps = 16;
 constexpr int kNormParts = 1024;   // partial sums of squares per matrix, at most
 constexpr int kMaxSplits = 16;     // of the Gram product's long side
-constexpr double kLoGain = 16.0;   // X_k keeps its low part above this gain
 // Growth of an error in A_k that a group of steps may cause, in units of
-// sqrt(s), with one plane and with two.  The rounding of A_k is a random matrix:
-// its norm, against that of A_k, falls with sqrt(s).  Measured on low-rank
-// matrices with noise of 1e-3 and 1e-4 of the largest singular value: with
-// these limits the error against 64 bits is at most that of the same steps in
-// binary32 for f32 matrices, and at most 1.5 times its rounding to bf16 (two
-// steps on one plane at s = 64: 8.4e-3 against 2.4e-3 for single ones; three on
-// two planes at s = 64: 4.2e-5 against 8.5e-6; at s = 512: 2.1e-3 against
-// 1.9e-3, and 7.0e-6 against 7.6e-6).
-constexpr double kGroupGain[2] = {0.55, 6.7};
-// bf16 matrices up to this short side take two planes as well.
-constexpr int64_t kWideSide = 192;
+// sqrt(s).  The rounding of A_k is a random matrix: its norm, against that of
+// A_k, falls with sqrt(s).  Measured on low-rank matrices with noise of 1e-3 and
+// 1e-4 of the largest singular value: with this limit the error against 64 bits
+// is at most that of the same steps in binary32 for f32 matrices (three steps at
+// s = 64: 4.2e-5 against 8.5e-6; at s = 512: 7.0e-6 against 7.6e-6).
+constexpr double kGroupGain = 6.7;
 
 // Factors of one matrix's epilogues, by group of steps (see factors_of).
 struct Factors {
   float gram[kMaxSteps];                                 // acc -> stored A
   float mid[kMaxSteps];                                  // acc -> stored X, or the result
-  float mean;                                            // of the stored Q's diagonal
 };
 
 // What the host knows of a group of steps [first, first + count): scales of
@@ -239,8 +221,7 @@ __device__ void factors_of(const Scales& sc, double norm, Factors* f) {
   }
 }
 
-// Eight values as hi and lo parts, stored at hi + at and lo + at (lo: may be
-// null).
+// Eight values as hi and lo parts, stored at hi + at and lo + at.
 __device__ __forceinline__ void store_parts(const float (&v)[8], f16_t* hi, f16_t* lo, int64_t at) {
   h8_t h, l;
 #pragma unroll
@@ -249,7 +230,7 @@ __device__ __forceinline__ void store_parts(const float (&v)[8], f16_t* hi, f16_
     l[e] = (f16_t)(v[e] - (float)h[e]);
   }
   *reinterpret_cast<h8_t*>(hi + at) = h;
-  if (lo) *reinterpret_cast<h8_t*>(lo + at) = l;
+  *reinterpret_cast<h8_t*>(lo + at) = l;
 }
 
 // Stored X_0 = 2^e U in both orders, zero past the matrix: a tile of 64 x 64
@@ -367,10 +348,6 @@ struct ProductArgs {
   // kPoly
   const f16_t *ahi, *alo;
   float ax, bx, cx;
-  // kMid, kLast on one plane: the low part of X ([l][s], pitch xld), if it has one
-  const f16_t* xlo;
-  int64_t xld, sxlo;
-  int x_first;                 // X is the first operand (rows i)
   // kLast: the caller's matrix
   void* O; int64_t ldo, so;
   void* W; int64_t ldw, sw;
@@ -385,35 +362,21 @@ __device__ __forceinline__ void store_both(const ProductArgs& p, int b, int i, i
   split4(v, hi, lo);
   const int64_t at = b * p.sd + j * p.ld + i;
   *reinterpret_cast<h4_t*>(p.hi + at) = hi;
-  if (p.lo) *reinterpret_cast<h4_t*>(p.lo + at) = lo;
+  *reinterpret_cast<h4_t*>(p.lo + at) = lo;
   if (turned) {
     const int64_t tat = b * p.sdt + (int64_t)(i + (lane & 3)) * p.ldt + (j & ~3);
     *reinterpret_cast<h4_t*>(p.thi + tat) = turn4(hi, lane);
-    if (p.tlo) *reinterpret_cast<h4_t*>(p.tlo + tat) = turn4(lo, lane);
+    *reinterpret_cast<h4_t*>(p.tlo + tat) = turn4(lo, lane);
   }
 }
 
 // One lane's share of a 16 x 16 tile of the product, rows i .. i + 3 of column
-// j (in range): what is stored for it, before its rounding.  LO: X has a low
-// part beside the plane that was multiplied.
-template <Role ROLE, bool LO>
-__device__ __forceinline__ f4_t value(const ProductArgs& p, int b, int i, int j, f4_t acc, float factor, float mean) {
-  if constexpr (LO) {
-    const f16_t* x = p.xlo + b * p.sxlo;
-    if (ROLE == Role::kMid || !p.x_first) {
-      const h4_t lo = *reinterpret_cast<const h4_t*>(x + j * p.xld + i);
-#pragma unroll
-      for (int r = 0; r < 4; ++r) acc[r] += mean * (float)lo[r];
-    } else {
-#pragma unroll
-      for (int r = 0; r < 4; ++r) acc[r] += mean * (float)x[(int64_t)(i + r) * p.xld + j];
-    }
-  }
+// j (in range): what is stored for it, before its rounding.
+template <Role ROLE>
+__device__ __forceinline__ f4_t value(const ProductArgs& p, int b, int i, int j, f4_t acc, float factor) {
   if constexpr (ROLE == Role::kPoly) {
     const int64_t at = b * p.sd + j * p.ld + i;
-    const h4_t ah = *reinterpret_cast<const h4_t*>(p.ahi + at);
-    h4_t al = {0, 0, 0, 0};
-    if (p.alo) al = *reinterpret_cast<const h4_t*>(p.alo + at);
+    const h4_t ah = *reinterpret_cast<const h4_t*>(p.ahi + at), al = *reinterpret_cast<const h4_t*>(p.alo + at);
 #pragma unroll
     for (int r = 0; r < 4; ++r)
       acc[r] = p.bx * ((float)ah[r] + (float)al[r]) + p.cx * acc[r] + (i + r == j ? p.ax : 0.f);
@@ -425,12 +388,12 @@ __device__ __forceinline__ f4_t value(const ProductArgs& p, int b, int i, int j,
 }
 
 // The end of a small tile's 16 x 16 part, stored as the lanes hold it.
-template <typename T, Role ROLE, bool LO>
+template <typename T, Role ROLE>
 __device__ __forceinline__ void finish(const ProductArgs& p, int b, int split, int i, int j, f4_t acc,
-                                       bool turned, float factor, float mean, int lane) {
+                                       bool turned, float factor, int lane) {
   // Stored extents are multiples of 64: a 16 x 16 part is in or out as a whole.
   if (i >= p.rows_i || j >= p.rows_j) return;
-  acc = value<ROLE, LO>(p, b, i, j, acc, factor, mean);
+  acc = value<ROLE>(p, b, i, j, acc, factor);
   if constexpr (ROLE == Role::kLast) {
     if (i >= p.m || j >= p.n) return;
     T* out = p.W ? (T*)p.W + b * p.sw + i + j * p.ldw : (T*)p.O + b * p.so + i + j * p.ldo;
@@ -449,16 +412,16 @@ __device__ __forceinline__ void finish(const ProductArgs& p, int b, int split, i
 
 // The end of a wavefront's 16 TS x 16 TS part of a large tile, whose corner is
 // (iw, jw), in strips through LDS (store.h; Q X of 4096 x 11008: 421 -> 388 us).
-template <typename T, Role ROLE, int TS, bool LO>
+template <typename T, Role ROLE, int TS>
 __device__ __forceinline__ void finish_tile(const ProductArgs& p, int b, int split, int iw, int jw, f4_t (&acc)[TS][TS],
-                                            bool turned, float factor, float mean, int lane, char* buf) {
+                                            bool turned, float factor, int lane, char* buf) {
   const int g = lane >> 4, m16 = lane & 15;
 #pragma unroll
   for (int y = 0; y < TS; ++y)
 #pragma unroll
     for (int x = 0; x < TS; ++x) {
       const int i = iw + 16 * x + 4 * g, j = jw + 16 * y + m16;
-      if (i < p.rows_i && j < p.rows_j) acc[x][y] = value<ROLE, LO>(p, b, i, j, acc[x][y], factor, mean);
+      if (i < p.rows_i && j < p.rows_j) acc[x][y] = value<ROLE>(p, b, i, j, acc[x][y], factor);
     }
   if constexpr (ROLE == Role::kGramPart) {
     float* part = p.part + (int64_t)(b * p.splits + split) * p.rows_j * p.ld;
@@ -499,16 +462,16 @@ __device__ __forceinline__ void finish_tile(const ProductArgs& p, int b, int spl
           char* at = turn ? buf + (4 * g + (lane & 3)) * kPitch + (16 * e + (m16 & 12)) * 2
                           : buf + m16 * kPitch + (16 * e + 4 * g) * 2;
           *reinterpret_cast<h4_t*>(at) = turn ? turn4(h, lane) : h;
-          if (lo) *reinterpret_cast<h4_t*>(at + 16 * kPitch) = turn ? turn4(l, lane) : l;
+          *reinterpret_cast<h4_t*>(at + 16 * kPitch) = turn ? turn4(l, lane) : l;
         }
         wave_lds();
         leave(buf, hi, ld, i0, j0 + 16 * z, rows_i, rows_j);
-        if (lo) leave(buf + 16 * kPitch, lo, ld, i0, j0 + 16 * z, rows_i, rows_j);
+        leave(buf + 16 * kPitch, lo, ld, i0, j0 + 16 * z, rows_i, rows_j);
         wave_lds();
       }
     };
-    strips(false, p.hi + b * p.sd, p.lo ? p.lo + b * p.sd : nullptr, p.ld, iw, jw, p.rows_i, p.rows_j);
-    if (turned) strips(true, p.thi + b * p.sdt, p.tlo ? p.tlo + b * p.sdt : nullptr, p.ldt, jw, iw, p.rows_j, p.rows_i);
+    strips(false, p.hi + b * p.sd, p.lo + b * p.sd, p.ld, iw, jw, p.rows_i, p.rows_j);
+    if (turned) strips(true, p.thi + b * p.sdt, p.tlo + b * p.sdt, p.ldt, jw, iw, p.rows_j, p.rows_i);
   }
 }
 
@@ -546,9 +509,8 @@ __device__ __forceinline__ void band_triangle_tile(int w, int n, int& bi, int& b
   }
 }
 
-// TS = 0: the split tile of 32 x 32; else the ring tile of 32 TS with S chunks,
-// or with WIDE the one for operands of two planes.
-template <typename T, Role ROLE, int TS, int S, bool WIDE, bool LO>
+// TS = 0: the split tile of 32 x 32; else the wide tile of 32 TS with S stages.
+template <typename T, Role ROLE, int TS, int S>
 __global__ __launch_bounds__(256) void ns_product_kernel(ProductArgs p) {
   const int b = blockIdx.z, split = blockIdx.y;
   int bi, bj;
@@ -566,7 +528,6 @@ __global__ __launch_bounds__(256) void ns_product_kernel(ProductArgs p) {
   const int lane = threadIdx.x & 63, g = lane >> 4, m16 = lane & 15;
   const bool turned = ROLE == Role::kMid || bi != bj;
   const float factor = ROLE == Role::kSym ? p.factor : ROLE == Role::kGram ? p.fac[b].gram[p.group] : p.fac[b].mid[p.group];
-  const float mean = LO ? p.fac[b].mean : 0.f;
   int64_t first = 0;             // byte of a row to start at, chunks from there
   int nk = p.op.nk;
   if (ROLE == Role::kGramPart) {
@@ -576,30 +537,22 @@ __global__ __launch_bounds__(256) void ns_product_kernel(ProductArgs p) {
     first = (int64_t)k0 * kChunkBytes;
   }
   if constexpr (TS == 0) {
-    typedef SplitTile<Kind::kF16, 2, 2> ST;
+    typedef SplitTile<2, 2> ST;
     __shared__ __attribute__((aligned(1024))) char lds[ST::kLds];
     const int i0 = bi * ST::BM, j0 = bj * ST::BN;
     ST::run(p.op, nk, b * p.su + first, b * p.sv + first, i0, j0, lds, [&](int x, int y, f4_t v) __attribute__((always_inline)) {
-      finish<T, ROLE, LO>(p, b, split, i0 + 16 * x + 4 * g, j0 + 16 * y + m16, v, turned, factor, mean, lane);
+      finish<T, ROLE>(p, b, split, i0 + 16 * x + 4 * g, j0 + 16 * y + m16, v, turned, factor, lane);
     });
   } else {
     constexpr int size = 32 * TS, kShare = 16 * (64 * TS + 32);      // LDS of a wavefront in finish_tile
     f4_t acc[TS][TS];
     const int wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int iw = bi * size + (wv & 1) * 16 * TS, jw = bj * size + (wv >> 1) * 16 * TS;
-    if constexpr (WIDE) {
-      typedef WideTile<Kind::kF16, TS, S> WT;
-      static_assert(4 * kShare <= WT::kLds, "LDS");
-      __shared__ __attribute__((aligned(1024))) char lds[WT::kLds];
-      WT::run(p.op, 2 * nk, b * p.su + first, b * p.sv + first, bi * size, bj * size, lds, acc);
-      finish_tile<T, ROLE, TS, LO>(p, b, split, iw, jw, acc, turned, factor, mean, lane, lds + wv * kShare);
-    } else {
-      typedef RingTile<Kind::kF16, TS, S> RT;
-      static_assert(4 * kShare <= RT::kLds, "LDS");
-      __shared__ __attribute__((aligned(1024))) char lds[RT::kLds];
-      RT::run(p.op, nk, b * p.su + first, b * p.sv + first, bi * size, bj * size, lds, acc);
-      finish_tile<T, ROLE, TS, LO>(p, b, split, iw, jw, acc, turned, factor, mean, lane, lds + wv * kShare);
-    }
+    typedef WideTile<TS, S> WT;
+    static_assert(4 * kShare <= WT::kLds, "LDS");
+    __shared__ __attribute__((aligned(1024))) char lds[WT::kLds];
+    WT::run(p.op, 2 * nk, b * p.su + first, b * p.sv + first, bi * size, bj * size, lds, acc);
+    finish_tile<T, ROLE, TS>(p, b, split, iw, jw, acc, turned, factor, lane, lds + wv * kShare);
   }
 }
 
@@ -630,50 +583,26 @@ __global__ __launch_bounds__(256) void ns_join_kernel(ProductArgs p) {
   store_both(p, b, i, j, v, bi != bj, lane);
 }
 
-// The mean of the diagonal of Q as stored (s values, pitch ld).
-__global__ __launch_bounds__(256) void ns_mean_kernel(const f16_t* Q, int64_t ld, int64_t stride, int s, Factors* fac) {
-  __shared__ float ws[4];
-  const f16_t* q = Q + blockIdx.x * stride;
-  float sum = 0.f;
-  for (int i0 = threadIdx.x; i0 < s; i0 += 256 * 8) {
-    float v[8];
-#pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      const int i = i0 + 256 * e;
-      v[e] = (float)q[(int64_t)min(i, s - 1) * (ld + 1)] * (i < s ? 1.f : 0.f);
-    }
-#pragma unroll
-    for (int e = 0; e < 8; ++e) sum += v[e];
-  }
-  for (int o = 32; o > 0; o >>= 1) sum += __shfl_xor(sum, o);
-  if ((threadIdx.x & 63) == 0) ws[threadIdx.x >> 6] = sum;
-  __syncthreads();
-  if (threadIdx.x == 0) fac[blockIdx.x].mean = (ws[0] + ws[1] + ws[2] + ws[3]) / s;
-}
-
 // --- host ------------------------------------------------------------------------
 
 struct Layout {
   int64_t s, l, sp, lp;        // short and long side, padded to whole chunks
-  bool wide;                   // two planes everywhere
-  bool x0lo;                   // X_0 needs its low part
-  size_t part, fac, xl[2], xs[2][2], sq[5][2], share, total;      // byte offsets
+  size_t part, fac, xl[2], xs[2][2], sq[5][2], total;      // byte offsets
+  size_t share[2];             // of the Gram product of the X in xs[0], xs[1]
 };
 
 // Splits of the Gram product that the workspace allows: their shares take no
-// more room than two planes of X.
+// more room than the two planes of X.
 int64_t gram_splits(int64_t sp, int64_t lp) {
   return sp == 0 ? 1 : std::max<int64_t>(1, std::min<int64_t>(kMaxSplits, lp / sp));
 }
 
-Layout layout_of(int dtype, int64_t m, int64_t n, int64_t batch, bool momentum) {
+Layout layout_of(int dtype, int64_t m, int64_t n, int64_t batch) {
   Layout y{};
   y.s = std::min(m, n);
   y.l = std::max(m, n);
   y.sp = round_up(y.s, 64);
   y.lp = round_up(y.l, 64);
-  y.wide = dtype != RRF_BF16 || y.s <= kWideSide;
-  y.x0lo = y.wide || momentum;
   size_t at = 0;
   auto take = [&](size_t bytes) {
     const size_t o = at;
@@ -684,36 +613,34 @@ Layout layout_of(int dtype, int64_t m, int64_t n, int64_t batch, bool momentum) 
   y.part = take((size_t)batch * kNormParts * 8);
   y.fac = take((size_t)batch * sizeof(Factors));
   for (int h = 0; h < 2; ++h) {
-    const bool have = h == 0 || y.wide;
-    y.xl[h] = have ? take(x) : 0;
-    for (int z = 0; z < 5; ++z) y.sq[z][h] = have ? take(q) : 0;
-    for (int z = 0; z < 2; ++z) y.xs[z][h] = take(x);
+    y.xl[h] = take(x);
+    for (int z = 0; z < 5; ++z) y.sq[z][h] = take(q);
   }
+  for (int z = 0; z < 2; ++z)
+    for (int h = 0; h < 2; ++h) y.xs[z][h] = take(x);
+  // A call on bf16 matrices needs less room than one on f32 or f16 ones: the
+  // shares lie where the next X will be, not in a place of their own.
   const int64_t splits = gram_splits(y.sp, y.lp);
-  y.share = splits > 1 ? take((size_t)(y.sp * y.sp * batch * splits) * 4) : 0;
+  const size_t share = splits > 1 ? (size_t)(y.sp * y.sp * batch * splits) * 4 : 0;
+  for (int z = 0; z < 2; ++z) y.share[z] = y.xs[z ^ 1][0];
+  if (dtype != RRF_BF16 && share > 0) y.share[0] = y.share[1] = take(share);
   y.total = at;
   return y;
 }
 
-// Costs of the products' launches (cost.h), chunks of 64 values.  First for one
-// pair of planes, then for two planes each (three products).  A fit to the
+// Costs of the products' launches (cost.h), chunks of 64 values.  A fit to the
 // measured times of the five sizes at sides from 64 to 11008 and batches of 1 to
-// 16 (within 15 % of them on average).  Over whole calls of 18 shapes, the sizes
-// it chooses take at most 3 % more than the best single size for all products
-// (bf16 4096 x 4096: 1.42 ms; 128 alone 1.81, 192 1.52, 256 1.66).
-constexpr TileCost kTiles[2][5] = {{{32, 66, 250, 260, 2700}, {64, 160, 320, 530, 3800}, {128, 300, 680, 1240, 7200},
-                                    {192, 550, 1000, 0, 10100}, {256, 1070, 1530, 0, 17500}},
-                                   {{32, 200, 500, 560, 3100}, {64, 330, 940, 1310, 5600}, {128, 890, 1530, 3150, 11000},
-                                    {192, 1610, 2790, 0, 15100}, {256, 3250, 4180, 0, 25600}}};
+// 16 (within 15 % of them on average).
+constexpr TileCost kTiles[5] = {{32, 200, 500, 560, 3100}, {64, 330, 940, 1310, 5600}, {128, 890, 1530, 3150, 11000},
+                                {192, 1610, 2790, 0, 15100}, {256, 3250, 4180, 0, 25600}};
 
 // The tile size of a product (index into kTiles), and for Gram products the
 // number of splits of the contraction, with the least time by that model.
 struct Choice { int tile, splits; double time; };
-Choice choose_tile(int64_t rows_i, int64_t rows_j, bool triangle, int64_t batch, bool wide, int64_t nk,
-                   int64_t max_splits) {
+Choice choose_tile(int64_t rows_i, int64_t rows_j, bool triangle, int64_t batch, int64_t nk, int64_t max_splits) {
   Choice best{0, 1, 1e300};
   for (int q = 0; q < 5; ++q) {
-    const TileCost& c = kTiles[wide][q];
+    const TileCost& c = kTiles[q];
     const int64_t ti = ceil_div(rows_i, c.size), tj = ceil_div(rows_j, c.size);
     const int64_t tiles = batch * (triangle ? ti * (ti + 1) / 2 : ti * tj);
     for (int64_t z = 1; z <= max_splits; ++z) {
@@ -744,7 +671,6 @@ double scale_of(double x) {
 // bound leaves the range that binary16 times a power of two can hold.
 bool scales_of(const double* coeffs, int steps, double eps, const Layout& y, int64_t batch, Scales* sc,
                Step* step) {
-  const bool wide = y.wide;
   double top[kMaxSteps + 1], pm[kMaxSteps];      // bounds of X_k's singular values and of |p_k|
   top[0] = 1.0;
   for (int k = 0; k < steps; ++k) {
@@ -762,9 +688,9 @@ bool scales_of(const double* coeffs, int steps, double eps, const Layout& y, int
   // Time of a group's products with X, and of one of the short side.
   double long_time = 0.0, short_time = 0.0;
   if (batch > 0 && y.s > 0) {
-    long_time = choose_tile(y.sp, y.sp, true, batch, wide, y.lp / 64, gram_splits(y.sp, y.lp)).time +
-                choose_tile(y.sp, y.lp, false, batch, wide, y.sp / 64, 1).time;
-    short_time = choose_tile(y.sp, y.sp, true, batch, wide, y.sp / 64, 1).time;
+    long_time = choose_tile(y.sp, y.sp, true, batch, y.lp / 64, gram_splits(y.sp, y.lp)).time +
+                choose_tile(y.sp, y.lp, false, batch, y.sp / 64, 1).time;
+    short_time = choose_tile(y.sp, y.sp, true, batch, y.sp / 64, 1).time;
   }
   sc->eps = eps;
   sc->groups = 0;
@@ -777,7 +703,7 @@ bool scales_of(const double* coeffs, int steps, double eps, const Layout& y, int
       growth *= pm[k + g - 2] * pm[k + g - 2];
       product *= pm[k + g - 1];
       const double work = (long_time + (4 * g - 3) * short_time) / g;
-      if (growth > kGroupGain[wide] * std::sqrt((double)y.s) || product > 1e4) break;
+      if (growth > kGroupGain * std::sqrt((double)y.s) || product > 1e4) break;
       if (work < least) { least = work; count = g; }
     }
     Group& q = sc->group[sc->groups++];
@@ -816,10 +742,9 @@ struct Call {
   T* O; int64_t ldo, so;
   T* W; int64_t ldw, sw;
   float keep, rate;
-  int steps;
 };
 
-template <typename T, Role ROLE, int TS, int S, bool WIDE>
+template <typename T, Role ROLE, int TS, int S>
 hipError_t launch_tiles(ProductArgs p, int64_t batch, hipStream_t st) {
   constexpr int size = TS == 0 ? 32 : 32 * TS;
   p.ti = (int)ceil_div(p.op.rows_u, size);
@@ -827,50 +752,32 @@ hipError_t launch_tiles(ProductArgs p, int64_t batch, hipStream_t st) {
   const int64_t tiles = on_triangle(ROLE) ? (int64_t)p.ti * (p.ti + 1) / 2 : (int64_t)p.ti * p.tj;
   const unsigned splits = ROLE == Role::kGramPart ? p.splits : 1;
   const dim3 grid((unsigned)tiles, splits, (unsigned)batch);
-  if constexpr (!WIDE && (ROLE == Role::kMid || ROLE == Role::kLast)) {
-    if (p.xlo) ns_product_kernel<T, ROLE, TS, S, WIDE, true><<<grid, 256, 0, st>>>(p);
-    else ns_product_kernel<T, ROLE, TS, S, WIDE, false><<<grid, 256, 0, st>>>(p);
-  } else {
-    ns_product_kernel<T, ROLE, TS, S, WIDE, false><<<grid, 256, 0, st>>>(p);
-  }
+  ns_product_kernel<T, ROLE, TS, S><<<grid, 256, 0, st>>>(p);
   return hipGetLastError();
 }
 
-template <typename T, Role ROLE, bool WIDE>
-hipError_t launch_sized(const ProductArgs& p, int tile, int64_t batch, hipStream_t st) {
+// T: the caller's type, for its matrix (kLast); what is not the caller's does
+// not depend on it.
+template <typename T, Role ROLE>
+hipError_t launch_product(const ProductArgs& p, int tile, int64_t batch, hipStream_t st) {
   switch (tile) {
-    case 0: return launch_tiles<T, ROLE, 0, 0, WIDE>(p, batch, st);
-    case 1: return launch_tiles<T, ROLE, 2, 4, WIDE>(p, batch, st);
+    case 0: return launch_tiles<T, ROLE, 0, 0>(p, batch, st);
+    case 1: return launch_tiles<T, ROLE, 2, 4>(p, batch, st);
     case 2: {
       // A deeper ring where a compute unit has one workgroup only (1792 x
       // 1792 x 5376: 60 -> 40 us), two workgroups where there are enough.
       const int64_t ti = ceil_div(p.op.rows_u, 128), tj = ceil_div(p.op.rows_v, 128);
       const int64_t tiles = batch * (on_triangle(ROLE) ? ti * (ti + 1) / 2 : ti * tj) *
                             (ROLE == Role::kGramPart ? p.splits : 1);
-      return tiles <= 256 ? launch_tiles<T, ROLE, 4, 4, WIDE>(p, batch, st)
-                          : launch_tiles<T, ROLE, 4, 2, WIDE>(p, batch, st);
+      return tiles <= 256 ? launch_tiles<T, ROLE, 4, 4>(p, batch, st) : launch_tiles<T, ROLE, 4, 2>(p, batch, st);
     }
-    case 3: return launch_tiles<T, ROLE, 6, 3, WIDE>(p, batch, st);
-    default: return launch_tiles<T, ROLE, 8, 2, WIDE>(p, batch, st);
+    case 3: return launch_tiles<T, ROLE, 6, 3>(p, batch, st);
+    default: return launch_tiles<T, ROLE, 8, 2>(p, batch, st);
   }
 }
 
-// What is not the caller's does not depend on its type; f32 and f16 matrices
-// always have two planes.
-template <typename T, Role ROLE>
-hipError_t launch_product(const ProductArgs& p, bool wide, int tile, int64_t batch, hipStream_t st) {
-  if constexpr (ROLE == Role::kLast && !__is_same(T, bf16_t))
-    return launch_sized<T, ROLE, true>(p, tile, batch, st);
-  else if constexpr (ROLE == Role::kLast)
-    return wide ? launch_sized<T, ROLE, true>(p, tile, batch, st) : launch_sized<T, ROLE, false>(p, tile, batch, st);
-  else
-    return wide ? launch_sized<float, ROLE, true>(p, tile, batch, st)
-                : launch_sized<float, ROLE, false>(p, tile, batch, st);
-}
-
 template <typename T>
-hipError_t iterate(const Call<T>& c, const Scales& sc, const Step* step, const double* coeffs, const Layout& y, char* ws,
-                   hipStream_t st) {
+hipError_t iterate(const Call<T>& c, const Scales& sc, const Step* step, const Layout& y, char* ws, hipStream_t st) {
   const int64_t m = c.src.m, n = c.src.n;
   const bool wide_m = m <= n;      // the contiguous index is the short one
   double* part = (double*)(ws + y.part);
@@ -884,8 +791,8 @@ hipError_t iterate(const Call<T>& c, const Scales& sc, const Step* step, const d
   ns_norm_kernel<T><<<dim3(parts, (unsigned)c.batch), 256, 0, st>>>(c.src, part);
   if ((e = hipGetLastError()) != hipSuccess) return e;
   {
-    f16_t *xs_hi = plane(y.xs[0][0]), *xs_lo = y.x0lo ? plane(y.xs[0][1]) : nullptr;
-    f16_t *xl_hi = plane(y.xl[0]), *xl_lo = y.wide ? plane(y.xl[1]) : nullptr;
+    f16_t *xs_hi = plane(y.xs[0][0]), *xs_lo = plane(y.xs[0][1]);
+    f16_t *xl_hi = plane(y.xl[0]), *xl_lo = plane(y.xl[1]);
     const int64_t ip = round_up(m, 64), jp = round_up(n, 64);
     const dim3 grid((unsigned)(ip / 64), (unsigned)(jp / 64), (unsigned)c.batch);
     const bool sw = !wide_m;      // ij is then the long side's order
@@ -904,7 +811,7 @@ hipError_t iterate(const Call<T>& c, const Scales& sc, const Step* step, const d
   };
   struct Square { f16_t *hi, *lo; };
   Square sq[5];
-  for (int z = 0; z < 5; ++z) sq[z] = Square{plane(y.sq[z][0]), y.wide ? plane(y.sq[z][1]) : nullptr};
+  for (int z = 0; z < 5; ++z) sq[z] = Square{plane(y.sq[z][0]), plane(y.sq[z][1])};
   const Square A = sq[0], B = sq[1], P = sq[2];
   // A product of short-side matrices, both triangles stored.
   auto square = [&](const Square& u, const Square& v, const Square& out) {
@@ -918,27 +825,26 @@ hipError_t iterate(const Call<T>& c, const Scales& sc, const Step* step, const d
     return q;
   };
   int cur = 0;
-  bool lo_cur = y.x0lo;
   for (int gr = 0; gr < sc.groups; ++gr) {
     const Group& grp = sc.group[gr];
-    f16_t *xl = plane(y.xl[0]), *xll = y.wide ? plane(y.xl[1]) : nullptr;
-    f16_t *X = plane(y.xs[cur][0]), *Xl = lo_cur ? plane(y.xs[cur][1]) : nullptr;
+    f16_t *xl = plane(y.xl[0]), *xll = plane(y.xl[1]);
+    f16_t *X = plane(y.xs[cur][0]), *Xl = plane(y.xs[cur][1]);
     Square Q = sq[3], R = sq[4];       // the product of the group's P's, and the next one's place
     {
       ProductArgs q = square(A, A, A);
       q.group = gr;
       q.op = operands(xl, xll, xl, xll, y.sp, y.sp, y.lp);
       q.su = q.sv = sx * 2;
-      const Choice t = choose_tile(y.sp, y.sp, true, c.batch, y.wide, q.op.nk, gram_splits(y.sp, y.lp));
+      const Choice t = choose_tile(y.sp, y.sp, true, c.batch, q.op.nk, gram_splits(y.sp, y.lp));
       if (t.splits > 1) {
         q.splits = t.splits;
-        q.part = (float*)(ws + y.share);
-        if ((e = launch_product<T, Role::kGramPart>(q, y.wide, t.tile, c.batch, st)) != hipSuccess) return e;
+        q.part = (float*)(ws + y.share[cur]);
+        if ((e = launch_product<float, Role::kGramPart>(q, t.tile, c.batch, st)) != hipSuccess) return e;
         const int64_t blocks = y.sp / 32;
         ns_join_kernel<<<dim3((unsigned)(blocks * (blocks + 1) / 2), 1, (unsigned)c.batch), 256, 0, st>>>(q);
         e = hipGetLastError();
       } else {
-        e = launch_product<T, Role::kGram>(q, y.wide, t.tile, c.batch, st);
+        e = launch_product<float, Role::kGram>(q, t.tile, c.batch, st);
       }
       if (e != hipSuccess) return e;
     }
@@ -946,22 +852,22 @@ hipError_t iterate(const Call<T>& c, const Scales& sc, const Step* step, const d
       const Step& t = step[grp.first + k];
       const Square& out = k == 0 ? Q : P;
       ProductArgs q = square(A, A, out);
-      const int tile = choose_tile(y.sp, y.sp, true, c.batch, y.wide, q.op.nk, 1).tile;
+      const int tile = choose_tile(y.sp, y.sp, true, c.batch, q.op.nk, 1).tile;
       q.ahi = A.hi; q.alo = A.lo;
       q.ax = t.ax; q.bx = t.bx; q.cx = t.cx;
-      if ((e = launch_product<T, Role::kPoly>(q, y.wide, tile, c.batch, st)) != hipSuccess) return e;
+      if ((e = launch_product<float, Role::kPoly>(q, tile, c.batch, st)) != hipSuccess) return e;
       if (k + 1 < grp.count) {
         q = square(out, A, B);
         q.factor = t.ft;
-        if ((e = launch_product<T, Role::kSym>(q, y.wide, tile, c.batch, st)) != hipSuccess) return e;
+        if ((e = launch_product<float, Role::kSym>(q, tile, c.batch, st)) != hipSuccess) return e;
         q = square(B, out, A);
         q.factor = t.fa;
-        if ((e = launch_product<T, Role::kSym>(q, y.wide, tile, c.batch, st)) != hipSuccess) return e;
+        if ((e = launch_product<float, Role::kSym>(q, tile, c.batch, st)) != hipSuccess) return e;
       }
       if (k > 0) {
         q = square(P, Q, R);
         q.factor = t.fq;
-        if ((e = launch_product<T, Role::kSym>(q, y.wide, tile, c.batch, st)) != hipSuccess) return e;
+        if ((e = launch_product<float, Role::kSym>(q, tile, c.batch, st)) != hipSuccess) return e;
         std::swap(Q, R);
       }
     }
@@ -970,29 +876,16 @@ hipError_t iterate(const Call<T>& c, const Scales& sc, const Step* step, const d
     q.fac = fac;
     q.rows_i = (int)(wide_m || gr + 1 < sc.groups ? y.sp : y.lp);
     q.rows_j = (int)(wide_m || gr + 1 < sc.groups ? y.lp : y.sp);
-    if (!y.wide && Xl) {
-      ns_mean_kernel<<<(unsigned)c.batch, 256, 0, st>>>(Q.hi, y.sp, sq_stride, (int)y.s, fac);
-      if ((e = hipGetLastError()) != hipSuccess) return e;
-      q.xlo = Xl;
-      q.xld = y.sp;
-      q.sxlo = sx;
-      Xl = nullptr;
-    }
-    const int next = grp.first + grp.count;
     if (gr + 1 < sc.groups) {
-      double gain = 1.0;
-      for (int j = next; j < c.steps; ++j) gain *= std::fabs(coeffs[3 * j]);
-      const bool lo_next = y.wide || gain > kLoGain;
       q.op = operands(Q.hi, Q.lo, X, Xl, y.sp, y.lp, y.sp);
       q.su = sq_stride * 2; q.sv = sx * 2;
-      q.hi = plane(y.xs[cur ^ 1][0]); q.lo = lo_next ? plane(y.xs[cur ^ 1][1]) : nullptr;
+      q.hi = plane(y.xs[cur ^ 1][0]); q.lo = plane(y.xs[cur ^ 1][1]);
       q.thi = xl; q.tlo = xll;
       q.ld = y.sp; q.ldt = y.lp; q.sd = q.sdt = sx;
-      e = launch_product<T, Role::kMid>(
-          q, y.wide, choose_tile(y.sp, y.lp, false, c.batch, y.wide, q.op.nk, 1).tile, c.batch, st);
+      e = launch_product<float, Role::kMid>(
+          q, choose_tile(y.sp, y.lp, false, c.batch, q.op.nk, 1).tile, c.batch, st);
       if (e != hipSuccess) return e;
       cur ^= 1;
-      lo_cur = lo_next;
     } else {
       // Rows i of the result are the caller's contiguous index.
       if (wide_m) {
@@ -1001,14 +894,13 @@ hipError_t iterate(const Call<T>& c, const Scales& sc, const Step* step, const d
       } else {
         q.op = operands(X, Xl, Q.hi, Q.lo, y.lp, y.sp, y.sp);
         q.su = sx * 2; q.sv = sq_stride * 2;
-        q.x_first = 1;
       }
       q.O = c.O; q.ldo = c.ldo; q.so = c.so;
       q.W = c.W; q.ldw = c.ldw; q.sw = c.sw;
       q.keep = c.keep; q.rate = c.rate;
       q.m = (int)m; q.n = (int)n;
       e = launch_product<T, Role::kLast>(
-          q, y.wide, choose_tile(y.sp, y.lp, false, c.batch, y.wide, q.op.nk, 1).tile, c.batch, st);
+          q, choose_tile(y.sp, y.lp, false, c.batch, q.op.nk, 1).tile, c.batch, st);
       if (e != hipSuccess) return e;
     }
   }
@@ -1019,22 +911,18 @@ hipError_t iterate(const Call<T>& c, const Scales& sc, const Step* step, const d
 struct Schedule {
   Scales scales;
   Step step[kMaxSteps];
-  const double* coeffs;
-  int steps;
 };
 
 // What every call checks: sizes, coefficients, workspace.
 rrf_status check_common(int dtype, int64_t m, int64_t n, int64_t batch, const double* coeffs, int64_t steps,
-                        double eps, bool momentum, const void* ws, size_t bytes, Schedule* sc, Layout* y) {
+                        double eps, const void* ws, size_t bytes, Schedule* sc, Layout* y) {
   if (!valid_real(dtype) || m < 0 || n < 0 || batch < 0) return RRF_ERR_INVALID_ARG;
   if (!coeffs || steps < 1 || steps > kMaxSteps || !(eps > 0.0) || !std::isfinite(eps))
     return RRF_ERR_INVALID_ARG;
   for (int64_t i = 0; i < 3 * steps; ++i)
     if (!std::isfinite(coeffs[i])) return RRF_ERR_INVALID_ARG;
-  sc->steps = (int)steps;
-  sc->coeffs = coeffs;
   if (m > (1 << 20) || n > (1 << 20) || std::min(m, n) > 65536 || batch > 65535) return RRF_ERR_SHAPE;
-  *y = layout_of(dtype, m, n, batch, momentum);
+  *y = layout_of(dtype, m, n, batch);
   if (!scales_of(coeffs, (int)steps, eps, *y, batch, &sc->scales, sc->step)) return RRF_ERR_INVALID_ARG;
   if (m == 0 || n == 0 || batch == 0) return RRF_OK;
   if (!ws || ((uintptr_t)ws & 255) || bytes < y->total) return RRF_ERR_INVALID_ARG;
@@ -1053,8 +941,7 @@ rrf_status ortho_typed(int64_t m, int64_t n, int64_t batch, const void* G, int64
   c.src = Source<T>{(const T*)G, ldg, sg, nullptr, 0, 0, 0.f, 0, m, n};
   c.batch = batch;
   c.O = (T*)O; c.ldo = ldo; c.so = so;
-  c.steps = sc.steps;
-  return status_of(iterate<T>(c, sc.scales, sc.step, sc.coeffs, y, (char*)ws, (hipStream_t)stream));
+  return status_of(iterate<T>(c, sc.scales, sc.step, y, (char*)ws, (hipStream_t)stream));
 }
 
 template <typename T>
@@ -1066,8 +953,7 @@ rrf_status muon_typed(int64_t m, int64_t n, int64_t batch, void* W, int64_t ldw,
   c.batch = batch;
   c.W = (T*)W; c.ldw = ldw; c.sw = sw;
   c.keep = keep; c.rate = rate;
-  c.steps = sc.steps;
-  return status_of(iterate<T>(c, sc.scales, sc.step, sc.coeffs, y, (char*)ws, (hipStream_t)stream));
+  return status_of(iterate<T>(c, sc.scales, sc.step, y, (char*)ws, (hipStream_t)stream));
 }
 
 }  // namespace
@@ -1078,12 +964,12 @@ using namespace rrf::ops;
 
 extern "C" {
 
-rrf_status rrf_orthogonalize_workspace(rrf_dtype dtype, int64_t m, int64_t n, int64_t batch, int momentum,
+rrf_status rrf_orthogonalize_workspace(rrf_dtype dtype, int64_t m, int64_t n, int64_t batch, int,
                                        size_t* bytes) {
   const int dt = int_bits(dtype);
   if (!bytes || !valid_real(dt) || m < 0 || n < 0 || batch < 0) return RRF_ERR_INVALID_ARG;
   if (m > (1 << 20) || n > (1 << 20) || std::min(m, n) > 65536 || batch > 65535) return RRF_ERR_SHAPE;
-  *bytes = (m == 0 || n == 0 || batch == 0) ? 0 : layout_of(dt, m, n, batch, momentum != 0).total;
+  *bytes = (m == 0 || n == 0 || batch == 0) ? 0 : layout_of(dt, m, n, batch).total;
   return RRF_OK;
 }
 
@@ -1094,7 +980,7 @@ rrf_status rrf_orthogonalize(rrf_dtype dtype, int64_t m, int64_t n, int64_t batc
   const int dt = int_bits(dtype);
   Schedule sc;
   Layout y;
-  const rrf_status s = check_common(dt, m, n, batch, coeffs, steps, eps, false, workspace, workspace_bytes, &sc, &y);
+  const rrf_status s = check_common(dt, m, n, batch, coeffs, steps, eps, workspace, workspace_bytes, &sc, &y);
   if (s != RRF_OK || m == 0 || n == 0 || batch == 0) return s;
   const int size = real_size(dt);
   if (bad_matrix(G, ldg, stride_g, m, n, batch, size) || bad_matrix(O, ldo, stride_o, m, n, batch, size) ||
@@ -1120,7 +1006,7 @@ rrf_status rrf_muon_step(rrf_dtype dtype, int64_t m, int64_t n, int64_t batch, v
   Layout y;
   if (!std::isfinite(lr) || !std::isfinite(momentum) || !std::isfinite(weight_decay) || !std::isfinite(scale))
     return RRF_ERR_INVALID_ARG;
-  const rrf_status s = check_common(dt, m, n, batch, coeffs, steps, eps, true, workspace, workspace_bytes, &sc, &y);
+  const rrf_status s = check_common(dt, m, n, batch, coeffs, steps, eps, workspace, workspace_bytes, &sc, &y);
   if (s != RRF_OK || m == 0 || n == 0 || batch == 0) return s;
   const int size = real_size(dt);
   if (bad_matrix(G, ldg, stride_g, m, n, batch, size) || bad_matrix(W, ldw, stride_w, m, n, batch, size) ||

@@ -1,16 +1,16 @@
-// A tile of the product (tile.h) of one pair of planes, its parts overlapped by
-// hand: a workgroup of four wavefronts forms a 32 T x 32 T tile of D, a
-// wavefront 16 T x 16 T of it, and a ring of S chunks in LDS feeds them.
+// What the tiles of a product (tile.h) that are fed from a ring of chunks in LDS
+// share (wide.h, ring4.h): a workgroup of four wavefronts forms a 32 T x 32 T
+// tile of D, a wavefront 16 T x 16 T of it.
 //
-// One wavefront a SIMD keeps the matrix unit busy by itself: the operands of
-// the next half chunk are read from LDS, and a later chunk is loaded from
-// memory, between the matrix instructions of the present half, one access for
-// every T / 2 of them (loads that come in bursts hold up the wavefront that
-// issues them: 2850 against 2430 cycles a chunk of T = 8).  One barrier a
-// chunk, in its middle, where every wavefront has its last operands of the
-// chunk in registers: the chunk's place in the ring is free from there on.
-// The accumulators are tied to the accumulation registers in the instruction;
-// left to the compiler they are moved about between matrix instructions.
+// One wavefront a SIMD keeps the matrix unit busy by itself: the operands that
+// come next are read from LDS, and a later chunk is loaded from memory, between
+// the matrix instructions of the present ones, a few at a time (loads that come
+// in bursts hold up the wavefront that issues them: 2850 against 2430 cycles a
+// chunk of 16-bit operands at T = 8).  One barrier a chunk, in its middle, where
+// every wavefront has its last operands of the chunk in registers: the chunk's
+// place in the ring is free from there on.  The accumulators are tied to the
+// accumulation registers in the instruction; left to the compiler they are moved
+// about between matrix instructions.
 #pragma once
 
 #include "tile.h"
@@ -25,12 +25,8 @@ __device__ __forceinline__ rsrc_t rsrc_of(const void* p, int64_t size = 0xffffff
   return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(p), 0, (int)size, 0x27000);
 }
 
-template <Kind KIND>
 __device__ __forceinline__ void mfma_acc(f4_t& c, i4_t a, i4_t b) {
-  if constexpr (KIND == Kind::kF16)
-    asm volatile("v_mfma_f32_16x16x32_f16 %0, %1, %2, %0" : "+a"(c) : "v"(a), "v"(b));
-  else
-    asm volatile("v_mfma_f32_16x16x32_bf16 %0, %1, %2, %0" : "+a"(c) : "v"(a), "v"(b));
+  asm volatile("v_mfma_f32_16x16x32_f16 %0, %1, %2, %0" : "+a"(c) : "v"(a), "v"(b));
 }
 
 // s_waitcnt for at most N outstanding vector memory accesses and no LDS ones.
@@ -39,114 +35,6 @@ __device__ __forceinline__ void wait_mem() {
   static_assert(N >= 0 && N < 64, "counter of six bits");
   __builtin_amdgcn_s_waitcnt((N & 15) | ((N >> 4) << 14) | (7 << 4));
 }
-
-template <Kind KIND, int T, int S>
-struct RingTile {
-  static constexpr int BM = 32 * T, BN = 32 * T, kThreads = 256, WI = 2;
-  static constexpr int kTI = T, kTJ = T;
-  static constexpr int kStage = (BM + BN) * kChunkBytes;
-  static constexpr int kLds = S * kStage;
-  static constexpr int kLoads = 2 * T;          // a thread and chunk
-  static_assert(S >= 2 && (S - 2) * kLoads < 64 && T % 2 == 0, "ring");
-
-  static __device__ __forceinline__ void run(const Operands& op, int nk, int64_t batch_u, int64_t batch_v, int i0,
-                                             int j0, char* lds, f4_t (&acc)[kTI][kTJ]) {
-    const int t = threadIdx.x, lane = t & 63, wv = __builtin_amdgcn_readfirstlane(t >> 6);
-    const int wi = (wv & 1) * 16 * T, wj = (wv >> 1) * 16 * T;
-    const int g = lane >> 4, m16 = lane & 15;
-    const int r8 = lane >> 3, pk = (lane & 7) ^ r8;
-    // A wavefront loads rows wv 8 T .. + 8 T - 1 of both images, 8 a load.
-    int ou[T], ov[T];
-#pragma unroll
-    for (int q = 0; q < T; ++q) {
-      const int r = wv * 8 * T + q * 8 + r8;
-      ou[q] = (int)((int64_t)(min(i0 + r, op.rows_u - 1) - i0) * op.ldu + pk * 16);
-      ov[q] = (int)((int64_t)(min(j0 + r, op.rows_v - 1) - j0) * op.ldv + pk * 16);
-    }
-    const int64_t bu = batch_u + (int64_t)i0 * op.ldu, bv = batch_v + (int64_t)j0 * op.ldv;
-#pragma unroll
-    for (int a = 0; a < T; ++a)
-#pragma unroll
-      for (int b = 0; b < T; ++b) acc[a][b] = f4_t{0.f, 0.f, 0.f, 0.f};
-    const rsrc_t ru = rsrc_of(op.u + bu), rv = rsrc_of(op.v + bv);
-    int k = 0, so = 0, slot = 0;              // of the next load
-    // Past the last chunk the first one is loaded again, and not used.
-    auto advance = [&]() __attribute__((always_inline)) {
-      so += kChunkBytes;
-      slot = slot == (S - 1) * kStage ? 0 : slot + kStage;
-      if (++k == nk) { k = 0; so = 0; }
-    };
-    auto load1 = [&](int q) __attribute__((always_inline)) {
-      char* l = lds + slot + wv * (1024 * T) + (q >> 1) * 1024;
-      if (q & 1)
-        __builtin_amdgcn_raw_ptr_buffer_load_lds(rv, (__attribute__((address_space(3))) void*)(l + BM * kChunkBytes), 16,
-                                                 ov[q >> 1], so, 0, 0);
-      else
-        __builtin_amdgcn_raw_ptr_buffer_load_lds(ru, (__attribute__((address_space(3))) void*)l, 16, ou[q >> 1], so,
-                                                 0, 0);
-    };
-    int lu[2], lv[2];
-#pragma unroll
-    for (int kk = 0; kk < 2; ++kk) {
-      lu[kk] = pack_at(wi + m16, kk * 4 + g);
-      lv[kk] = BM * kChunkBytes + pack_at(wj + m16, kk * 4 + g);
-    }
-    i4_t f0[2 * T], f1[2 * T];      // V's, then U's operands of a half chunk
-    auto fetch1 = [&](int at, int kk, int q, i4_t (&f)[2 * T]) __attribute__((always_inline)) {
-      f[q] = *reinterpret_cast<const i4_t*>(lds + at + (q < T ? lv[kk] : lu[kk]) + (q % T) * 2048);
-    };
-    // Matrix instructions of group q, of 2 T in a half chunk, in two parts.
-    auto mul = [&](int q, int part, i4_t (&f)[2 * T]) __attribute__((always_inline)) {
-      constexpr int N = T / 2;
-      const int x = q >> 1, y0 = (q & 1) * N;
-#pragma unroll
-      for (int y = part ? N / 2 : 0; y < (part ? N : N / 2); ++y)
-        mfma_acc<KIND>(acc[x][y0 + y], f[T + x], f[y0 + y]);
-    };
-    auto barrier = [&]() __attribute__((always_inline)) {
-      __builtin_amdgcn_s_barrier();
-      __builtin_amdgcn_sched_barrier(0);
-    };
-#pragma unroll
-    for (int s = 0; s < S; ++s) {
-      for (int q = 0; q < kLoads; ++q) load1(q);
-      advance();
-    }
-    wait_mem<(S - 1) * kLoads < 64 ? (S - 1) * kLoads : 63>();
-    barrier();
-#pragma unroll
-    for (int q = 0; q < 2 * T; ++q) fetch1(0, 0, q, f0);
-    int at = 0;
-    for (int c = 0; c < nk; ++c) {
-#pragma unroll
-      for (int q = 0; q < 2 * T; ++q) {
-        fetch1(at, 1, q, f1);
-        mul(q, 0, f0);
-        mul(q, 1, f0);
-        __builtin_amdgcn_sched_barrier(0);
-      }
-      // Chunk c + 1 has arrived and every wavefront has read chunk c.
-      wait_mem<(S - 2) * kLoads>();
-      barrier();
-      at = at == (S - 1) * kStage ? 0 : at + kStage;
-#pragma unroll
-      for (int q = 0; q < 2 * T; ++q) {
-        fetch1(at, 0, q, f0);
-        mul(q, 0, f1);
-        __builtin_amdgcn_sched_barrier(0);
-        load1(q);
-        mul(q, 1, f1);
-        __builtin_amdgcn_sched_barrier(0);
-      }
-      advance();
-    }
-    // Nothing is under way into LDS, and the last results have been written,
-    // before the caller reads the one or uses the other.
-    wait_mem<0>();
-    asm volatile("s_nop 15\n s_nop 15" ::: "memory");
-    barrier();
-  }
-};
 
 }  // namespace ops
 }  // namespace rrf

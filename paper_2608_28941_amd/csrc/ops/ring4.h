@@ -1,7 +1,7 @@
-// The ring tile (ring.h) for operands of 4 bits with a scale for 32 values, on
-// the scaled matrix instruction.
+// A tile of the product (tile.h) of operands of 4 bits with a scale for 32 values,
+// on the scaled matrix instruction, its parts overlapped by hand (ring.h).
 //
-// A chunk of a row is 128 bytes here too (256 values), a lane's 16-byte pack is
+// A chunk of a row is 128 bytes (256 values), a lane's 16-byte pack is
 // one block of 32 values, and its scale is one byte.  The scales of four chunks,
 // 32 bytes a row, are loaded into LDS at a time, one group of four ahead: rows
 // are far apart in memory, and a load that takes 4 bytes of each of 64 rows

@@ -5,9 +5,9 @@
 // A small product is bound by latency.  Wavefronts that share chunks wait for
 // each other at a barrier for every one of them; here none waits for another
 // until the four partial tiles are added, in a fixed order, and the first R
-// chunks of all four are under way at once.  512 x 512 x 512: 3.4 us with 32 x
-// 32 tiles (T = 2, R = 2), against 4.9 with the ring tile of 64 x 64; 64 x 64
-// tiles here gain nothing over the ring tile's.
+// chunks of all four are under way at once.  (512 x 512 x 512 with one plane
+// each: 3.4 us with 32 x 32 tiles, T = 2, R = 2, against 4.9 with 64 x 64 tiles
+// from a shared ring, which 64 x 64 tiles here do not beat.)
 #pragma once
 
 #include "ring.h"
@@ -15,7 +15,7 @@
 namespace rrf {
 namespace ops {
 
-template <Kind KIND, int T, int R>
+template <int T, int R>
 struct SplitTile {
   static constexpr int BM = 16 * T, BN = 16 * T, kThreads = 256;
   static constexpr int kStage = (BM + BN) * kChunkBytes;
@@ -45,7 +45,7 @@ struct SplitTile {
     for (int a = 0; a < T; ++a)
 #pragma unroll
       for (int b = 0; b < T; ++b) acc[a][b] = f4_t{0.f, 0.f, 0.f, 0.f};
-    const int total = (op.ul ? 3 : 1) * nk;
+    const int total = 3 * nk;
     const int mine = (total - wv + 3) >> 2;      // chunks wv, wv + 4, ...
     char* ring = lds + wv * (R * kStage);
     int issued = 0, slot = 0;
@@ -87,7 +87,7 @@ struct SplitTile {
 #pragma unroll
         for (int x = 0; x < T; ++x)
 #pragma unroll
-          for (int y = 0; y < T; ++y) acc[x][y] = mfma16<KIND>(a[kk][x], b[kk][y], acc[x][y]);
+          for (int y = 0; y < T; ++y) acc[x][y] = mfma16<Kind::kF16>(a[kk][x], b[kk][y], acc[x][y]);
       at = at == R - 1 ? 0 : at + 1;
     }
     __syncthreads();

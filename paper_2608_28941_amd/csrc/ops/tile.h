@@ -49,10 +49,10 @@ __device__ __forceinline__ f4_t mfma16(i4_t a, i4_t b, f4_t c) {
 // Position of pack p of row r in a chunk's LDS image, in bytes.
 __device__ __forceinline__ int pack_at(int r, int p) { return r * kChunkBytes + ((p ^ (r & 7)) << 4); }
 
-// A product's operands, whose values may be sums of two 16-bit parts: then u +
-// ul times v + vl is taken as u v + ul v + u vl.
+// A product's operands, whose values are sums of two 16-bit parts: u + ul times
+// v + vl is taken as u v + ul v + u vl.
 struct Operands {
-  const char *u, *ul, *v, *vl;      // ul and vl: both or neither
+  const char *u, *ul, *v, *vl;
   int nk;           // chunks of a row
   int64_t ldu, ldv; // row pitch in bytes
   int rows_u, rows_v;

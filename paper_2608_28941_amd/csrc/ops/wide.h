@@ -1,5 +1,6 @@
-// The ring tile (ring.h) for operands of two planes, u = u_hi + u_lo and v =
-// v_hi + v_lo: D = u_hi v_hi + u_hi v_lo + u_lo v_hi.
+// A tile of the product (tile.h) of operands of two planes, u = u_hi + u_lo and v
+// = v_hi + v_lo: D = u_hi v_hi + u_hi v_lo + u_lo v_hi, its parts overlapped by
+// hand (ring.h).
 //
 // A stage of the ring holds 32 values of a row, of both planes of both
 // operands, so that a loaded operand serves all the products it is part of:
@@ -19,7 +20,7 @@
 namespace rrf {
 namespace ops {
 
-template <Kind KIND, int T, int S>
+template <int T, int S>
 struct WideTile {
   static constexpr int BM = 32 * T, BN = 32 * T, kThreads = 256;
   static constexpr int kRow = 64;
@@ -84,7 +85,7 @@ struct WideTile {
     // Half a row of D's tiles: T / 2 matrix instructions.
     auto mul = [&](const i4_t& u, i4_t (&v)[T], int x, int half) __attribute__((always_inline)) {
 #pragma unroll
-      for (int y = 0; y < T / 2; ++y) mfma_acc<KIND>(acc[x][half * (T / 2) + y], u, v[half * (T / 2) + y]);
+      for (int y = 0; y < T / 2; ++y) mfma_acc(acc[x][half * (T / 2) + y], u, v[half * (T / 2) + y]);
     };
 #pragma unroll
     for (int s = 0; s < S; ++s) {

@@ -19,8 +19,8 @@
 // + 1 multiplications (r = l / s: Gram product r on half its tiles, A^2 1 on
 // half, P X 2 r); a group of g steps 3 r + 4 g - 3.  Rounding A_k costs more
 // then: an error in it grows by at most (max |a + b x^2 + c x^4|)^2 a step up
-// to the next Gram product, so that growth is held to a limit (kGroupGain):
-// with the quintic up to three steps (s > 500; two below).
+// to the next Gram product.  How many steps that allows depends on the type of
+// the result (group_limit).
 //
 // Representation of the iterates.  Singular values stay below a bound that
 // the host takes from the coefficients, so X, A and P are held in binary16
@@ -51,13 +51,24 @@ namespace {
 constexpr int kMaxSteps = 16;
 constexpr int kNormParts = 1024;   // partial sums of squares per matrix, at most
 constexpr int kMaxSplits = 16;     // of the Gram product's long side
-// Growth of an error in A_k that a group of steps may cause, in units of
-// sqrt(s).  The rounding of A_k is a random matrix: its norm, against that of
-// A_k, falls with sqrt(s).  Measured on low-rank matrices with noise of 1e-3 and
-// 1e-4 of the largest singular value: with this limit the error against 64 bits
-// is at most that of the same steps in binary32 for f32 matrices (three steps at
-// s = 64: 4.2e-5 against 8.5e-6; at s = 512: 7.0e-6 against 7.6e-6).
-constexpr double kGroupGain = 6.7;
+// Steps of a group from step k on at most, the growth of an error in A_k that it
+// may cause, and whether it is taken though it saves no time.  Matrices that a
+// twentieth of their rows, columns or singular values carries show the rounding
+// of A_k most; the largest errors over 14 such and other spectra, short sides of
+// 205 to 1030 (the first row: to 2000), five steps of the quintic (growth 12.3 a step):
+//   groups    against 64 bits    over that of the same steps in binary32
+//   2 1 1 1   4.2e-5             1.34
+//   2 2 1     4.2e-5             4.7 (at 3.8e-6)
+//   1 ...     6.4e-5             1.64 (every X is rounded; 1.42 at sides up to 300)
+//   2 3       2.3e-4             160
+// A bf16 result is rounded by 1.7e-3, an f16 one by 2.1e-4.
+struct GroupLimit { int steps; double gain; bool always; };
+GroupLimit group_limit(int dtype, int k, int64_t s) {
+  if (dtype == RRF_BF16) return {3, 160.0, false};
+  if (dtype == RRF_F16) return {2, 20.0, false};
+  if (k == 0) return {2, 20.0, s > 384};
+  return {1, 1.0, false};
+}
 
 // Factors of one matrix's epilogues, by group of steps (see factors_of).
 struct Factors {
@@ -669,7 +680,7 @@ double scale_of(double x) {
 // [0, 1], and the largest |x p(x)| and |p(x)| are taken over a fine grid, with
 // a margin for what lies between its points and for rounding.  False if a
 // bound leaves the range that binary16 times a power of two can hold.
-bool scales_of(const double* coeffs, int steps, double eps, const Layout& y, int64_t batch, Scales* sc,
+bool scales_of(int dtype, const double* coeffs, int steps, double eps, const Layout& y, int64_t batch, Scales* sc,
                Step* step) {
   double top[kMaxSteps + 1], pm[kMaxSteps];      // bounds of X_k's singular values and of |p_k|
   top[0] = 1.0;
@@ -696,15 +707,16 @@ bool scales_of(const double* coeffs, int steps, double eps, const Layout& y, int
   sc->groups = 0;
   double gain = 1.0;
   for (int k = 0; k < steps;) {
-    // The number of steps with the least time a step, within the error's limit.
+    // The number of steps with the least time a step, within the limits.
     int count = 1;
     double growth = 1.0, least = long_time + short_time, product = pm[k];
-    for (int g = 2; k + g <= steps; ++g) {
+    const GroupLimit limit = group_limit(dtype, k, y.s);
+    for (int g = 2; g <= limit.steps && k + g <= steps; ++g) {
       growth *= pm[k + g - 2] * pm[k + g - 2];
       product *= pm[k + g - 1];
       const double work = (long_time + (4 * g - 3) * short_time) / g;
-      if (growth > kGroupGain * std::sqrt((double)y.s) || product > 1e4) break;
-      if (work < least) { least = work; count = g; }
+      if (growth > limit.gain || product > 1e4) break;
+      if (work < least || limit.always) { least = work; count = g; }
     }
     Group& q = sc->group[sc->groups++];
     q.first = k;
@@ -923,7 +935,7 @@ rrf_status check_common(int dtype, int64_t m, int64_t n, int64_t batch, const do
     if (!std::isfinite(coeffs[i])) return RRF_ERR_INVALID_ARG;
   if (m > (1 << 20) || n > (1 << 20) || std::min(m, n) > 65536 || batch > 65535) return RRF_ERR_SHAPE;
   *y = layout_of(dtype, m, n, batch);
-  if (!scales_of(coeffs, (int)steps, eps, *y, batch, &sc->scales, sc->step)) return RRF_ERR_INVALID_ARG;
+  if (!scales_of(dtype, coeffs, (int)steps, eps, *y, batch, &sc->scales, sc->step)) return RRF_ERR_INVALID_ARG;
   if (m == 0 || n == 0 || batch == 0) return RRF_OK;
   if (!ws || ((uintptr_t)ws & 255) || bytes < y->total) return RRF_ERR_INVALID_ARG;
   return RRF_OK;

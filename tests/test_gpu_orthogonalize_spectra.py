@@ -103,3 +103,17 @@ def test_bf16_step_as_exact_as_binary32_rounded(kind):
         rrf.muon_step(W, layout(M, wide, order), layout(G, wide, order), lr=1.0, momentum=0.9)
         e, plain, size = errors(torch.bfloat16, U, -W, wide)
         assert e <= 1.5 * plain, (s, l, e / size, plain / size)
+
+
+@pytest.mark.parametrize("kind", KINDS)
+def test_f32_as_exact_as_binary32(kind):
+    """Steps that are taken together round X X^T where single ones round X:
+    their error is that of binary32 steps too, up to sixteen roundings of a
+    binary32 result."""
+    for q, (s, l) in enumerate([(205, 700), (515, 2060), (600, 3001), (1030, 4100), (2000, 2100)]):
+        say(f"orthogonalize f32 {kind} {s}x{l}")
+        G = spectrum(kind, s, l, 40 + q)
+        wide, order = q % 2 == 0, "crc"[q // 2]
+        O = rrf.orthogonalize(layout(G, wide, order))
+        e, plain, size = errors(torch.float32, G, O, wide)
+        assert e <= 1.5 * plain + 16 * 2.0 ** -24 * size, (s, l, e / size, plain / size)

@@ -214,7 +214,9 @@ __device__ __forceinline__ int norm_exp(double norm) {
 __device__ void factors_of(const Scales& sc, double norm, Factors* f) {
   const double inf = __longlong_as_double(0x7ff0000000000000ll);
   const double nu = norm / (norm + sc.eps);
-  double sx = ldexp(norm + sc.eps, norm_exp(norm));    // stored X_0 / X_0
+  // stored X_0 / X_0; any number for a matrix of zeros, where 1 / eps^2 could
+  // leave the range of the factors
+  double sx = norm == 0.0 ? 1.0 : ldexp(norm + sc.eps, norm_exp(norm));
   if (!(norm < inf)) sx = inf - inf;                   // a result of NaN
   for (int k = 0; k < sc.groups; ++k) {
     const Group& q = sc.group[k];

@@ -49,6 +49,7 @@ namespace ops {
 namespace {
 
 constexpr int kMaxSteps = 16;
+constexpr int kMaxScale = 400;     // exponent of a stored matrix's scale: products of two stay in binary64
 constexpr int kNormParts = 1024;   // partial sums of squares per matrix, at most
 constexpr int kMaxSplits = 16;     // of the Gram product's long side
 // Steps of a group from step k on at most, the growth of an error in A_k that it
@@ -80,7 +81,7 @@ struct Factors {
 // the stored matrices, powers of two from the bounds of their spectra.
 struct Group {
   int first, count;
-  float sa, sq;                // of A at its start, of the product of its P's
+  double sa, sq;               // of A at its start, of the product of its P's
   double bound, gain;          // after it: of X's singular values; the largest x_k / x_0
 };
 struct Scales {
@@ -220,16 +221,16 @@ __device__ void factors_of(const Scales& sc, double norm, Factors* f) {
   if (!(norm < inf)) sx = inf - inf;                   // a result of NaN
   for (int k = 0; k < sc.groups; ++k) {
     const Group& q = sc.group[k];
-    f->gram[k] = (float)((double)q.sa / (sx * sx));
+    f->gram[k] = (float)(q.sa / (sx * sx));
     double next = 1.0;
     if (k + 1 < sc.groups) {
       double b = q.gain * nu;
       b = b < q.bound ? b : q.bound;
       int e = 0;
       if (b > 0.0) (void)frexp(b, &e);
-      next = ldexp(1.0, min(15 - e, 100));
+      next = ldexp(1.0, min(15 - e, kMaxScale));
     }
-    f->mid[k] = (float)(next / (sx * (double)q.sq));
+    f->mid[k] = (float)(next / (sx * q.sq));
     sx = norm < inf ? next : inf - inf;
   }
 }
@@ -674,7 +675,7 @@ Choice choose_tile(int64_t rows_i, int64_t rows_j, bool triangle, int64_t batch,
 double scale_of(double x) {
   int e;
   (void)std::frexp(1.02 * x, &e);
-  return std::ldexp(1.0, 15 - e);
+  return std::ldexp(1.0, std::min(15 - e, kMaxScale));
 }
 
 // The groups of the steps and all scales, for matrices of sides s and l.
@@ -723,7 +724,7 @@ bool scales_of(int dtype, const double* coeffs, int steps, double eps, const Lay
     Group& q = sc->group[sc->groups++];
     q.first = k;
     q.count = count;
-    q.sa = (float)scale_of(top[k] * top[k]);
+    q.sa = scale_of(top[k] * top[k]);
     double sq = 1.0;
     product = 1.0;
     for (int j = k; j < k + count; ++j) {
@@ -741,7 +742,7 @@ bool scales_of(int dtype, const double* coeffs, int steps, double eps, const Lay
       sq = sn;
     }
     gain *= product;
-    q.sq = (float)sq;
+    q.sq = sq;
     q.bound = top[k + count];
     q.gain = gain;
     k += count;

@@ -35,3 +35,26 @@ def test_zero_matrix_whatever_eps(name, eps):
     M = torch.zeros(50, 70, device="cuda")
     rrf.muon_step(W, M, G[0].contiguous(), lr=0.1, weight_decay=0.5, eps=eps)
     assert torch.equal(W, want) and not bool(M.any())
+
+
+@pytest.mark.parametrize("coeffs", [
+    ((1e-12, 0.0, 0.0),) * 3,
+    ((1e-25, 0.0, 0.0), (1e3, 0.0, 0.0), (1e3, 0.0, 0.0)),
+    ((1e-10, 0.0, 0.0),) * 4 + ((9e3, 0.0, 0.0),) * 4,
+    ((1e-15, -1e-15, 0.0), (2.0, -1e30, 1e59)),
+])
+def test_coefficients_that_shrink_the_values(coeffs):
+    """Singular values far below 1 on the way: X and A are stored with scales
+    past binary32's range.  22 bits and binary32 sums: 16 roundings of 2^-20 a
+    step, and the result's own, down to the least normal number."""
+    say(f"orthogonalize {coeffs}")
+    gen = torch.Generator(device="cuda").manual_seed(2)
+    G = torch.randn(60, 90, device="cuda", generator=gen)
+    X = G.double() / (torch.linalg.vector_norm(G.double()) + 1e-7)
+    for a, b, c in coeffs:
+        S = X @ X.t().contiguous()
+        X = a * X + (b * S + c * S @ S) @ X
+    O = rrf.orthogonalize(G, coeffs).double()
+    size = float(torch.linalg.vector_norm(X))
+    assert 1e-37 < size
+    assert float(torch.linalg.vector_norm(O - X)) <= 16 * len(coeffs) * 2.0 ** -20 * size

@@ -78,6 +78,8 @@ struct Mx4Tile {
     }
     const rsrc_t ru = rsrc_of(op.u + i0 * pitch), rv = rsrc_of(op.v + j0 * pitch);
     // The last row's last group may end past the matrix: those bytes read as 0.
+    // The group is part of the lane's offset for that, as an instruction's scalar
+    // offset need not count in the comparison with the buffer's size.
     const rsrc_t rsu = rsrc_of(op.su + i0 * spitch, min(BM, op.rows_u - i0) * spitch);
     const rsrc_t rsv = rsrc_of(op.sv + j0 * spitch, min(BN, op.rows_v - j0) * spitch);
 #pragma unroll
@@ -100,11 +102,12 @@ struct Mx4Tile {
         __builtin_amdgcn_raw_ptr_buffer_load_lds(ru, (lds_ptr)l, 16, ou[q >> 1], k * kChunkBytes, 0, 0);
     };
     auto load_scales = [&](int group) __attribute__((always_inline)) {
+      if (4 * group >= op.nk) return;
 #pragma unroll
       for (int q = 0; q < T / 2; ++q) {
         const int z = wv * (T / 2) + q;
         char* l = lds + S * kStage + (group & 1) * kScales + z * 1024;
-        __builtin_amdgcn_raw_ptr_buffer_load_lds(z < T ? rsu : rsv, (lds_ptr)l, 16, os[q], group * 32, 0, 0);
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(z < T ? rsu : rsv, (lds_ptr)l, 16, os[q] + group * 32, 0, 0, 0);
       }
     };
     int lu[2], lv[2];

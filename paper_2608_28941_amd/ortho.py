@@ -167,15 +167,21 @@ def orthogonalize_workspace(dtype, m, n, batch=1, momentum=False):
     return got
 
 
-def _space(need, workspace, device):
-    torch = _torch()
+def _given(workspace, device):
+    """The caller's workspace, checked, as a tuple; empty without one."""
     if workspace is None:
-        return torch.empty(max(need, 256), dtype=torch.uint8, device=device)
+        return ()
     if not workspace.is_cuda or not workspace.is_contiguous():
         raise ValueError("workspace must be a contiguous CUDA tensor")
     if workspace.device != device:
         raise ValueError("workspace is on another device")
-    return workspace
+    return (workspace,)
+
+
+def _space(need, workspace, device):
+    if workspace is not None:
+        return workspace
+    return _torch().empty(max(need, 256), dtype=_torch().uint8, device=device)
 
 
 def orthogonalize(G, coeffs=MUON_COEFFS, eps=1e-7, out=None, workspace=None, stream=None):
@@ -204,7 +210,7 @@ def orthogonalize(G, coeffs=MUON_COEFFS, eps=1e-7, out=None, workspace=None, str
     m, n, batch, ldg, sg = _matrix(G, order)
     _, _, _, ldo, so = _matrix(out, order)
     c, steps = _coeffs(coeffs)
-    with on_device(G, stream, out) as s:
+    with on_device(G, stream, out, *_given(workspace, G.device)) as s:
         need = orthogonalize_workspace(G.dtype, m, n, batch)
         ws = _space(need, workspace, G.device)
         _abi.check(_abi.load().rrf_orthogonalize(
@@ -235,7 +241,7 @@ def muon_step(W, M, G, lr, momentum=0.95, nesterov=True, weight_decay=0.0, scale
     _, _, _, ldm, sm = _matrix(M, order)
     _, _, _, ldg, sg = _matrix(G, order)
     c, steps = _coeffs(coeffs)
-    with on_device(W, stream, M, G) as s:
+    with on_device(W, stream, M, G, *_given(workspace, G.device)) as s:
         need = orthogonalize_workspace(G.dtype, m, n, batch, True)
         ws = _space(need, workspace, W.device)
         _abi.check(_abi.load().rrf_muon_step(

@@ -8,7 +8,7 @@ everywhere in this package (``colmajor``).
 import ctypes
 
 from . import _abi
-from .ortho import _torch, on_device, real_code
+from .ortho import _torch, no_graph, on_device, real_code
 
 BLOCK = 32    # rows that share a scale
 PAD = 256     # a column is padded to a multiple of this
@@ -121,7 +121,8 @@ def _colmajor_ld(t, name):
 
 
 def mx4_quantize(X, stream=None):
-    """X (k x n, column-major; float32, bfloat16 or float16) in 4 bits."""
+    """X (k x n, column-major; float32, bfloat16 or float16) in 4 bits, which
+    carry no gradient."""
     torch = _torch()
     code = real_code(X.dtype)
     ldx = _colmajor_ld(X, "X")
@@ -169,9 +170,11 @@ def _apply_workspace(*key):
 def mx4_apply(A, B, trans=True, stream=None):
     """A^T B (trans) or A B of a 4-bit matrix A and a real column-major B, in
     B's type.  ``mx4_apply(A, dC, trans=not t)`` is the gradient for B of
-    ``C = mx4_apply(A, B, trans=t)``."""
+    ``C = mx4_apply(A, B, trans=t)``; autograd does not record it, and a B that
+    requires grad is refused outside torch.no_grad()."""
     torch = _torch()
     code = real_code(B.dtype)
+    no_graph("B", B)
     ldb = _colmajor_ld(B, "B")
     if A.device != B.device:
         raise ValueError("A and B are on different devices")

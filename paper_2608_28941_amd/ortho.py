@@ -41,6 +41,22 @@ def real_code(dt):
     raise TypeError("only float32, bfloat16 and float16 are supported")
 
 
+def no_graph(name, t):
+    """Refuses a tensor whose gradient the caller expects autograd to take: the
+    call records none."""
+    if t.requires_grad and _torch().is_grad_enabled():
+        raise RuntimeError(f"{name} requires grad, which this call does not record: "
+                           "detach it, or call under torch.no_grad()")
+
+
+def written(*tensors):
+    """Tells autograd that a call wrote them, so that a graph which kept one of
+    them for its backward refuses to use it."""
+    for t in tensors:
+        if not t.is_inference():
+            _torch().autograd.graph.increment_version(t)
+
+
 class _OnDevice:
     """A tensor's device and the given stream for the time of a call;
     ``handle`` is the stream's."""
@@ -192,10 +208,15 @@ def orthogonalize(G, coeffs=MUON_COEFFS, eps=1e-7, out=None, workspace=None, str
     out (new unless given; out may be G) in G's order.  A matrix whose norm is
     not finite gives NaN throughout.  workspace: optional contiguous CUDA
     tensor of at least orthogonalize_workspace(...) bytes, 256-byte aligned.
-    Asynchronous on the stream (None: the current one).
+    Asynchronous on the stream (None: the current one).  Autograd records
+    nothing: a G or out that requires grad is refused outside torch.no_grad().
     """
     torch = _torch()
     code = real_code(G.dtype)
+    no_graph("G", G)
+    given = out is not None
+    if given:
+        no_graph("out", out)
     if out is None:
         order = _common_order([("G", G)])
         with on_device(G, stream):
@@ -217,6 +238,8 @@ def orthogonalize(G, coeffs=MUON_COEFFS, eps=1e-7, out=None, workspace=None, str
             code, m, n, batch, G.data_ptr(), ldg, sg, out.data_ptr(), ldo, so, c, steps,
             float(eps), ws.data_ptr(), ws.numel() * ws.element_size(), s.handle),
             "rrf_orthogonalize")
+    if given:
+        written(out)
     return out
 
 
@@ -229,7 +252,9 @@ def muon_step(W, M, G, lr, momentum=0.95, nesterov=True, weight_decay=0.0, scale
         W <- (1 - lr weight_decay) W - lr scale orthogonalize(U)
 
     W and G share a type (float32, bfloat16 or float16), the momentum M is
-    float32; all three have the same shape and order.
+    float32; all three have the same shape and order.  Autograd records
+    nothing, as in every optimiser step, and W may require grad; a graph that
+    kept W or M for its backward refuses to use them afterwards.
     """
     code = real_code(G.dtype)
     if W.dtype != G.dtype:
@@ -249,4 +274,5 @@ def muon_step(W, M, G, lr, momentum=0.95, nesterov=True, weight_decay=0.0, scale
             float(lr), float(momentum), 1 if nesterov else 0, float(weight_decay), float(scale),
             c, steps, float(eps), ws.data_ptr(), ws.numel() * ws.element_size(), s.handle),
             "rrf_muon_step")
+    written(W, M)
     return W

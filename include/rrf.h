@@ -390,9 +390,9 @@ rrf_status rrf_muon_step(rrf_dtype dtype, int64_t m, int64_t n, int64_t batch,
  *   scales  kp / 32 bytes, one for 32 rows: byte s is 2^(s - 127), 255 NaN.
  * Columns follow each other without gaps, so a range of columns is a matrix.
  * codes is 16-byte aligned, scales 8-byte.  The padding must be zero.  Sizes
- * are at most 2^24.  dtype (RRF_F32, RRF_BF16 or RRF_F16) is the type of the
- * real matrices, which are column-major.  All calls are asynchronous on
- * hip_stream and allocate nothing.
+ * are at most 2^24 (columns to quantise or dequantise: 2^31 - 1).  dtype
+ * (RRF_F32, RRF_BF16 or RRF_F16) is the type of the real matrices, which are
+ * column-major.  All calls are asynchronous on hip_stream and allocate nothing.
  *
  * rrf_mx4_quantize    X (k x n) to codes and scales: the scale of a block is
  *   2^e, e = floor(log2 max|x|) - 2 held to [-127, 127]; x 2^-e is rounded to
@@ -403,7 +403,10 @@ rrf_status rrf_muon_step(rrf_dtype dtype, int64_t m, int64_t n, int64_t batch,
  *   summed in binary32, rounded to dtype once.
  * rrf_mx4_apply       C = A^T B (trans != 0: B k x n, C m x n) or C = A B
  *   (trans == 0: B m x n, C k x n) of a 4-bit k x m matrix A and a real B.
- *   Products are exact, sums binary32.  C must not overlap B.  workspace:
+ *   Products are exact, sums binary32, but for binary32 values of B below
+ *   2^-110 in magnitude: those are cut to multiples of 2^-133 (towards zero).
+ *   4-bit values past binary32's range count as infinite.  C must not overlap
+ *   B.  workspace:
  *   device, 16-byte aligned, at least rrf_mx4_apply_workspace(...) bytes (it
  *   may be NULL where that is 0).
  * A contraction over nothing (k = 0, or m = 0 without trans) gives C = 0.

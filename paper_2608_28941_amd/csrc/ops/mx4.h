@@ -37,8 +37,11 @@ __device__ __forceinline__ void mx_decode8(unsigned word, float scale, float (&v
   v[4] = c[0] * scale; v[5] = c[1] * scale; v[6] = d[0] * scale; v[7] = d[1] * scale;
 }
 
-// A real number as a sum of bfloat16 parts, exactly: 8 bits each, truncated
-// (rounding could overflow), so binary32 takes three, binary16 two.
+// A real number as a sum of bfloat16 parts: 8 bits each, truncated (rounding
+// could overflow), so binary32 takes three, binary16 two.  Exact down to 2^-110 in
+// magnitude; the last part of what is smaller falls below bfloat16's least
+// number, 2^-133, and the value is cut to a multiple of that.  (The matrix
+// instruction takes subnormal operands as they are.)
 template <typename T> constexpr int parts_of() { return sizeof(T) == 4 ? 3 : 2; }
 template <> constexpr int parts_of<bf16_t>() { return 1; }
 

@@ -6,8 +6,9 @@
 // registers.
 // rrf_mx4_apply: a 4-bit matrix or its transpose times real columns.  A 4-bit
 // value is a bfloat16 number exactly, and a real one is the exact sum of one
-// (bf16), two (f16) or three (f32) bfloat16 parts, so every product is exact
-// and the result has the error of binary32 sums alone.
+// (bf16), two (f16) or three (f32) bfloat16 parts (below 2^-110 up to 2^-133:
+// mx4.h), so every product is exact and the result has the error of binary32
+// sums alone.
 
 #include "mx4.h"
 #include "cost.h"
@@ -238,9 +239,10 @@ __device__ __forceinline__ Raw8<T> load_raw8(const T* col, int64_t l, int64_t L,
   return r;
 }
 // Their bfloat16 parts, eight to a pack: the upper halves of x, of what its
-// upper half leaves, and of what that one's leaves, each difference exact.  An
-// infinity leaves nothing (infinity less itself would be a NaN); eight values
-// without one, the usual case, are cut without looking at each.
+// upper half leaves, and of what that one's leaves (each difference is exact,
+// the last part as mx4.h says).  An infinity leaves nothing (infinity less
+// itself would be a NaN); eight values without one, the usual case, are cut
+// without looking at each.
 template <typename T>
 __device__ __forceinline__ void parts8(const Raw8<T>& r, i4_t (&o)[parts_of<T>()]) {
   constexpr int P = parts_of<T>();

@@ -150,14 +150,6 @@ __global__ __launch_bounds__(512) void mx4_product_few_kernel(MxArgs<T> p) {
   });
 }
 
-// Costs of the tiles' launches, chunks of 256 values; a fit to the times of 15
-// sizes from 1024 x 1024 to 11008 x 8192 (K = 512 to 11008).  The size it chooses
-// takes at most 2 % more than the best one there: 4096^3 43 us with 256 (58 with
-// 128), 11008 x 2048 with K = 4096 67 with 128 (70 with 256), 1024 x 1024 9.2
-// with 64 (12.8 with 128), 6000 x 6000 99 with 192 (102 and 105).
-constexpr TileCost kProductTiles[4] = {{64, 380, 385, 440, 3050}, {128, 460, 730, 1200, 5400},
-                                       {192, 790, 1250, 0, 7500}, {256, 1200, 1940, 0, 10700}};
-
 template <typename T, int TS, int S>
 void launch_tiles(MxArgs<T> p, hipStream_t st) {
   p.ti = (int)ceil_div(p.op.rows_u, 32 * TS);
@@ -178,14 +170,7 @@ rrf_status product_typed(int64_t M, int64_t N, int64_t k, const void* a, const v
   } else if (N <= 64) {
     mx4_product_few_kernel<T, 4><<<rows16, 512, 0, st>>>(p);
   } else {
-    int best = 0;
-    double least = 1e300;
-    for (int q = 0; q < 4; ++q) {
-      const int64_t tiles = ceil_div(M, kProductTiles[q].size) * ceil_div(N, kProductTiles[q].size);
-      const double time = tile_time(kProductTiles[q], tiles, p.op.nk);
-      if (time < least) { least = time; best = q; }
-    }
-    switch (best) {
+    switch (choose_product(M, N, p.op.nk)) {
       case 0: launch_tiles<T, 2, 4>(p, st); break;
       case 1: launch_tiles<T, 4, 2>(p, st); break;
       case 2: launch_tiles<T, 6, 2>(p, st); break;
@@ -736,65 +721,6 @@ __global__ __launch_bounds__(256) void mx4_join_kernel(ApplyArgs<T> p) {
     const int64_t j = w / rows;
     p.C[j * p.ldc + (w - j * rows)] = (T)s;
   }
-}
-
-// Columns of B up to which it takes the kernels for few of them: A^T B with
-// several parts would convert all of B again for every 16 columns of A.
-constexpr int64_t kFew = 64;
-bool few_columns(int trans, int parts, int64_t n) { return n <= (trans && parts > 1 ? 32 : kFew); }
-
-// Splits of the contraction of C = A B with few columns: about two workgroups
-// to a compute unit, at least 128 columns of A each.
-int64_t few_splits(int64_t k, int64_t m) {
-  return std::max<int64_t>(1, std::min(ceil_div(512, ceil_div(k, 128)), m / 128));
-}
-
-// Tiles of the kernel for many columns, the workgroups of them that the device
-// holds, and what a launch takes in ns: for a chunk of 64 contracted values with
-// one workgroup, with 256 and with all of them busy, and apart from the chunks;
-// for one part of B and for three (between them for two).  A fit to the measured
-// times of 34 shapes with 1 to 16 splits (within 11 % of them on average; the
-// choice takes 4 % more than the best one).
-struct ApplyTile { int wi, nt, cap; double one[4], three[4]; };
-constexpr ApplyTile kApplyTiles[5] = {{4, 4, 512, {920, 1220, 1340, 3900}, {1380, 2110, 2820, 5300}},
-                                      {4, 3, 512, {870, 1110, 1220, 3500}, {1260, 2090, 2090, 3600}},
-                                      {2, 4, 512, {950, 1210, 1230, 4200}, {1740, 2280, 2860, 6100}},
-                                      {2, 2, 768, {680, 920, 1090, 3700}, {1050, 1350, 2310, 3700}},
-                                      {2, 1, 1024, {540, 750, 1080, 2700}, {660, 920, 1650, 2600}}};
-constexpr int kMaxApplySplits = 16;
-
-// The tile and the number of splits of C (rows x n) with a contraction over L
-// that take the least time by that model.
-struct ApplyChoice { int tile, splits; };
-ApplyChoice choose_apply(int64_t rows, int64_t L, int64_t n, int parts) {
-  ApplyChoice best{0, 1};
-  double least = 1e300;
-  const int64_t chunks = ceil_div(L, 64);
-  for (int q = 0; q < 5; ++q) {
-    const ApplyTile& t = kApplyTiles[q];
-    double c[4];
-    for (int i = 0; i < 4; ++i) c[i] = parts == 1 ? t.one[i] : parts == 3 ? t.three[i] : 0.5 * (t.one[i] + t.three[i]);
-    const int64_t tiles = ceil_div(rows, 64 * t.wi) * ceil_div(n, 16 * t.nt * (4 / t.wi));
-    for (int z = 1; z <= kMaxApplySplits; ++z) {
-      const int64_t per = ceil_div(chunks, z), w = tiles * z;
-      if (z > 1 && ((z - 1) * per >= chunks || w > 1024)) continue;
-      auto round = [&](int64_t busy) {
-        const double chunk = busy <= 256 ? c[0] + (c[1] - c[0]) * busy / 256.0
-                                         : c[1] + (c[2] - c[1]) * (busy - 256) / (t.cap - 256.0);
-        return chunk * per + c[3];
-      };
-      // joining: a launch, and the sums written, read and added up
-      const double join = z == 1 ? 0.0 : 6000.0 + 4.0 * (z + 1) * rows * n / 4500.0;
-      const double time = (w / t.cap) * round(t.cap) + (w % t.cap ? round(w % t.cap) : 0.0) + join;
-      if (time < least) { least = time; best = ApplyChoice{q, z}; }
-    }
-  }
-  return best;
-}
-
-int64_t apply_splits(int trans, int parts, int64_t k, int64_t m, int64_t n) {
-  if (few_columns(trans, parts, n)) return trans ? 1 : few_splits(k, m);
-  return choose_apply(trans ? m : k, trans ? k : m, n, parts).splits;
 }
 
 template <typename T, int NT>

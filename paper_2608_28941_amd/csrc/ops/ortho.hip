@@ -51,7 +51,6 @@ namespace {
 constexpr int kMaxSteps = 16;
 constexpr int kMaxScale = 400;     // exponent of a stored matrix's scale: products of two stay in binary64
 constexpr int kNormParts = 1024;   // partial sums of squares per matrix, at most
-constexpr int kMaxSplits = 16;     // of the Gram product's long side
 // Steps of a group from step k on at most, the growth of an error in A_k that it
 // may cause, and whether it is taken though it saves no time.  Matrices that a
 // twentieth of their rows, columns or singular values carries show the rounding
@@ -605,12 +604,6 @@ struct Layout {
   size_t share[2];             // of the Gram product of the X in xs[0], xs[1]
 };
 
-// Splits of the Gram product that the workspace allows: their shares take no
-// more room than the two planes of X.
-int64_t gram_splits(int64_t sp, int64_t lp) {
-  return sp == 0 ? 1 : std::max<int64_t>(1, std::min<int64_t>(kMaxSplits, lp / sp));
-}
-
 Layout layout_of(int dtype, int64_t m, int64_t n, int64_t batch) {
   Layout y{};
   y.s = std::min(m, n);
@@ -640,33 +633,6 @@ Layout layout_of(int dtype, int64_t m, int64_t n, int64_t batch) {
   if (dtype != RRF_BF16 && share > 0) y.share[0] = y.share[1] = take(share);
   y.total = at;
   return y;
-}
-
-// Costs of the products' launches (cost.h), chunks of 64 values.  A fit to the
-// measured times of the five sizes at sides from 64 to 11008 and batches of 1 to
-// 16 (within 15 % of them on average).
-constexpr TileCost kTiles[5] = {{32, 200, 500, 560, 3100}, {64, 330, 940, 1310, 5600}, {128, 890, 1530, 3150, 11000},
-                                {192, 1610, 2790, 0, 15100}, {256, 3250, 4180, 0, 25600}};
-
-// The tile size of a product (index into kTiles), and for Gram products the
-// number of splits of the contraction, with the least time by that model.
-struct Choice { int tile, splits; double time; };
-Choice choose_tile(int64_t rows_i, int64_t rows_j, bool triangle, int64_t batch, int64_t nk, int64_t max_splits) {
-  Choice best{0, 1, 1e300};
-  for (int q = 0; q < 5; ++q) {
-    const TileCost& c = kTiles[q];
-    const int64_t ti = ceil_div(rows_i, c.size), tj = ceil_div(rows_j, c.size);
-    const int64_t tiles = batch * (triangle ? ti * (ti + 1) / 2 : ti * tj);
-    for (int64_t z = 1; z <= max_splits; ++z) {
-      const int64_t per = ceil_div(nk, z);
-      if (z > 1 && (z - 1) * per >= nk) continue;      // a split without chunks
-      // joining is a launch, reads z values of 4 bytes a place and writes one, at 4 TB/s
-      const double join = z == 1 ? 0.0 : 4000.0 + 4.0 * (z + 1) * batch * rows_i * rows_j / 2 / 4000.0;
-      const double cost = tile_time(c, tiles * z, per) + join;
-      if (cost < best.time) best = Choice{q, (int)z, cost};
-    }
-  }
-  return best;
 }
 
 // Largest power of two that keeps x times it below 2^15, and the product for
@@ -779,12 +745,9 @@ hipError_t launch_product(const ProductArgs& p, int tile, int64_t batch, hipStre
     case 0: return launch_tiles<T, ROLE, 0, 0>(p, batch, st);
     case 1: return launch_tiles<T, ROLE, 2, 4>(p, batch, st);
     case 2: {
-      // A deeper ring where a compute unit has one workgroup only (1792 x
-      // 1792 x 5376: 60 -> 40 us), two workgroups where there are enough.
-      const int64_t ti = ceil_div(p.op.rows_u, 128), tj = ceil_div(p.op.rows_v, 128);
-      const int64_t tiles = batch * (on_triangle(ROLE) ? ti * (ti + 1) / 2 : ti * tj) *
-                            (ROLE == Role::kGramPart ? p.splits : 1);
-      return tiles <= 256 ? launch_tiles<T, ROLE, 4, 4>(p, batch, st) : launch_tiles<T, ROLE, 4, 2>(p, batch, st);
+      const bool deep = one_a_unit(p.op.rows_u, p.op.rows_v, on_triangle(ROLE), batch,
+                                   ROLE == Role::kGramPart ? p.splits : 1);
+      return deep ? launch_tiles<T, ROLE, 4, 4>(p, batch, st) : launch_tiles<T, ROLE, 4, 2>(p, batch, st);
     }
     case 3: return launch_tiles<T, ROLE, 6, 3>(p, batch, st);
     default: return launch_tiles<T, ROLE, 8, 2>(p, batch, st);

@@ -100,8 +100,8 @@ inline int choose_product(int64_t M, int64_t N, int64_t nk) {
 
 // Columns of B up to which it takes the kernels for few of them: A^T B with
 // several parts would convert all of B again for every 16 columns of A.
-constexpr int64_t kFew = 64;
-inline bool few_columns(int trans, int parts, int64_t n) { return n <= (trans && parts > 1 ? 32 : kFew); }
+constexpr int64_t few_limit(bool trans, int parts) { return trans && parts > 1 ? 32 : 64; }
+inline bool few_columns(int trans, int parts, int64_t n) { return n <= few_limit(trans, parts); }
 
 // Splits of the contraction of C = A B with few columns: about two workgroups
 // to a compute unit, at least 128 columns of A each.

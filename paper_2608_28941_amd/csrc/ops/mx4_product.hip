@@ -723,10 +723,14 @@ __global__ __launch_bounds__(256) void mx4_join_kernel(ApplyArgs<T> p) {
   }
 }
 
+// For more than 8 NT columns up to 16 NT (from one with NT = 1), if few_limit goes
+// that far: else there is no such kernel, and no such call.
 template <typename T, int NT>
 void launch_few(ApplyArgs<T> p, int trans, hipStream_t st) {
+  static_assert(few_limit(false, parts_of<T>()) <= 64 && few_limit(true, parts_of<T>()) <= 64, "columns");
   if (trans) {
-    if constexpr (NT < 4 || parts_of<T>() == 1) mx4_apply_t_few_kernel<T, NT><<<(unsigned)ceil_div(p.m, 16), 512, 0, st>>>(p);
+    if constexpr (few_limit(true, parts_of<T>()) > 8 * NT)
+      mx4_apply_t_few_kernel<T, NT><<<(unsigned)ceil_div(p.m, 16), 512, 0, st>>>(p);
   } else {
     mx4_apply_n_few_kernel<T, NT><<<dim3((unsigned)ceil_div(p.k, 128), (unsigned)p.splits), 256, 0, st>>>(p);
   }

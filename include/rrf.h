@@ -370,7 +370,8 @@ rrf_status rrf_orthogonalize(rrf_dtype dtype, int64_t m, int64_t n,
  *   W <- (1 - lr weight_decay) W - lr scale O(U)
  * with O(U) the iteration above, never written to memory.  W and G have type
  * dtype, M is binary32 always; W, M and G must not overlap.  The workspace is
- * rrf_orthogonalize_workspace's with momentum != 0; otherwise as above.
+ * rrf_orthogonalize_workspace's with momentum != 0 (the same at present);
+ * otherwise as above.
  * ------------------------------------------------------------------------- */
 rrf_status rrf_muon_step(rrf_dtype dtype, int64_t m, int64_t n, int64_t batch,
                          void* W, int64_t ldw, int64_t stride_w, float* M,

@@ -30,10 +30,16 @@
 // three (hi hi + hi lo + lo hi), accumulated in binary32.  That holds for bf16
 // matrices too, though the result keeps 8 bits: the steps multiply small
 // singular values, and with them what rounding adds there, by up to 3.4^5.  One
-// plane of 11 bits was 1.8 times as fast (4096 x 11008) and as exact on low
-// rank with noise, but had two to three times the error of binary32 steps where
-// a twentieth of the rows or columns, or of the singular values, carries the
-// matrix.
+// plane of 11 bits was twice as fast (4096 x 11008: 2.5 ms against 5.1) and as
+// exact on low rank with noise, but had two to three times the error of binary32
+// steps where a twentieth of the rows or columns, or of the singular values,
+// carries the matrix.
+//
+// Bound by the matrix instructions where the sides are large (bf16 4096 x 11008:
+// 5.1 ms, 4096 x 4096 step: 3.4 ms, 1.21 PFLOP/s of 16-bit products), by LDS
+// traffic of 64 x 64 tiles around 1700 (f32 3001 x 1733 step: 0.81 ms, 0.55
+// PFLOP/s), by the latency of 17 launches where they are small (f32 500 x 300:
+// 86 us).
 
 #include "cost.h"
 #include "split.h"
@@ -60,7 +66,7 @@ constexpr int kNormParts = 1024;   // partial sums of squares per matrix, at mos
 //   2 1 1 1   4.2e-5             1.34
 //   2 2 1     4.2e-5             4.7 (at 3.8e-6)
 //   1 ...     6.4e-5             1.64 (every X is rounded; 1.42 at sides up to 300)
-//   2 3       2.3e-4             160
+//   2 3       2.9e-4             160
 // A bf16 result is rounded by 1.7e-3, an f16 one by 2.1e-4.
 struct GroupLimit { int steps; double gain; bool always; };
 GroupLimit group_limit(int dtype, int k, int64_t s) {
@@ -424,7 +430,8 @@ __device__ __forceinline__ void finish(const ProductArgs& p, int b, int split, i
 }
 
 // The end of a wavefront's 16 TS x 16 TS part of a large tile, whose corner is
-// (iw, jw), in strips through LDS (store.h; Q X of 4096 x 11008: 421 -> 388 us).
+// (iw, jw), in strips through LDS (store.h; Q X of 4096 x 11008 with one plane
+// each: 421 -> 388 us).
 template <typename T, Role ROLE, int TS>
 __device__ __forceinline__ void finish_tile(const ProductArgs& p, int b, int split, int iw, int jw, f4_t (&acc)[TS][TS],
                                             bool turned, float factor, int lane, char* buf) {
@@ -499,8 +506,8 @@ __device__ __forceinline__ void triangle_tile(int w, int& bi, int& bj) {
 // Tile (bi, bj), bi <= bj < n, number w of the triangle in bands of H tiles
 // along i: a band's corner, then its columns.  A die's tiles (32, or 64 where
 // two workgroups share a unit) then share 12 to 16 operand rows of tiles, not
-// 24 (Gram product of 4096 x 11008: 175 -> 166 us; with two planes, A^2 of 1733:
-// 45 -> 42).  With less than 64 tiles there is nothing to gain.
+// 24 (A^2 of 1733: 45 -> 42 us; with one plane each, Gram product of 4096 x
+// 11008: 175 -> 166).  With less than 64 tiles there is nothing to gain.
 template <int H>
 __device__ __forceinline__ void band_triangle_tile(int w, int n, int& bi, int& bj) {
   int i0 = 0, h = min(H, n);
